@@ -1,5 +1,5 @@
 """The calls that the rotary embedding and the 8-bit KV cache are timed on: what a step's queries, keys and values go
-through on their way into a cache of e4m3 codes with one scale per row, and out of it again.
+through on their way into a cache of e4m3 codes with one power of two per row, and out of it again.
 
 A case is a plain dict:
 
@@ -138,12 +138,13 @@ def _trees(case, rng):
 
 
 def _quantise(x):
-    """e4m3 codes and scales of the rows of x (finite values, float32): x is about codes * scales."""
+    """e4m3 codes and e8m0 scales of the rows of x (finite values, float32): x is about codes * scales."""
     top = x.abs().amax(-1)
     m, e = torch.frexp(top)
     e = (e - torch.where(m <= 0.875, 9, 8)).clamp_min(-126)          # 448 is 0.875 * 2^9
-    s = torch.where(top > 0, torch.ldexp(torch.ones_like(top), e), 1.0)
-    return (x / s[..., None]).to(torch.float8_e4m3fn), s
+    e = torch.where(top > 0, e, 0)
+    codes = (x / torch.ldexp(torch.ones_like(top), e)[..., None]).to(torch.float8_e4m3fn)
+    return codes, (e + 127).to(torch.uint8).view(torch.float8_e8m0fnu)
 
 
 def prepare(case, seed):
@@ -187,7 +188,7 @@ def prepare(case, seed):
     for x in ("k", "v"):
         if op == "append":                                  # a fresh pool
             s[x + "c"] = torch.zeros(shape, dtype=torch.float8_e4m3fn, device=dev)
-            s[x + "s"] = torch.zeros(shape[:3], device=dev)
+            s[x + "s"] = torch.full(shape[:3], 127, dtype=torch.uint8, device=dev).view(torch.float8_e8m0fnu)
         else:
             rows = torch.randn(shape, generator=gen, device=dev)
             rows *= torch.exp(0.3 * torch.randn(shape[:3], generator=gen, device=dev))[..., None]
@@ -257,7 +258,8 @@ def _rows(s, pos):
 
 def _gathered(codes, scales, page, slot):
     """Rows [B, n, Hkv, D] of the cache, float32."""
-    return codes.view(torch.uint8)[page, :, slot].view(torch.float8_e4m3fn).float() * scales[page, :, slot][..., None]
+    scale = scales.view(torch.uint8)[page, :, slot].view(torch.float8_e8m0fnu).float()
+    return codes.view(torch.uint8)[page, :, slot].view(torch.float8_e4m3fn).float() * scale[..., None]
 
 
 def _plain(s):
@@ -275,9 +277,8 @@ def _plain(s):
             k = _rotate(k, pos, s["freqs"], case["interleaved"])
         page, slot = _rows(s, s["lens"].long()[:, None] + torch.arange(T, device=dev))
         for rows, codes, scales in ((k, s["kc"], s["ks"]), (s["v"], s["vc"], s["vs"])):
-            c, sc = _quantise(rows.float())
-            codes.view(torch.uint8)[page, :, slot] = c.view(torch.uint8)
-            scales[page, :, slot] = sc
+            for x, held in zip(_quantise(rows.float()), (codes, scales)):
+                held.view(torch.uint8)[page, :, slot] = x.view(torch.uint8)
         return out + [s["kc"], s["ks"], s["vc"], s["vs"]]
     if op == "read":
         n = s["k_out"].shape[1]
@@ -294,8 +295,9 @@ def _plain(s):
         lens = s["lens"].long()[:, None]
         sp, ss = _rows(s, lens + torch.where(live, s["paths"].long(), 0))
         dp, ds = _rows(s, lens + torch.where(live, at, 0))              # (an entry past the path's end: the root onto itself)
-        for codes in (s["kc"].view(torch.uint8), s["vc"].view(torch.uint8), s["ks"], s["vs"]):
-            codes[dp, :, ds] = codes[sp, :, ss]
+        for x in (s["kc"], s["vc"], s["ks"], s["vs"]):
+            x = x.view(torch.uint8)
+            x[dp, :, ds] = x[sp, :, ss]
         s["lens_out"].copy_(s["lens"] + s["n_acc"])
         return [s["kc"], s["ks"], s["vc"], s["vs"], s["lens_out"]]
     lens = s["lens"].long()
@@ -357,7 +359,7 @@ def work(case):
     op, B, Hq, Hkv, D, T, ps = (case[k] for k in ("op", "B", "Hq", "Hkv", "D", "T", "ps"))
     es = 2 if case["dtype"] == "bf16" else 4
     lens = _lengths(case)
-    row = Hkv * (D + 4) * 2                                 # a token's codes and scales
+    row = Hkv * (D + 1) * 2                                 # a token's codes and scales
     dense = Hkv * D * es
     meta = 4 * B + (4 * B * T if case["tree"] == "dynamic" else 4 * T)
     if op == "rope":
@@ -423,7 +425,8 @@ def exact(case, seed):
 
     def values(c, sc, b, pos):
         page, slot = place(b, pos)
-        return c.view(torch.uint8)[page, :, slot].view(torch.float8_e4m3fn).double() * sc[page, :, slot].double()[..., None]
+        power = sc.view(torch.uint8)[page, :, slot].double() - 127.0
+        return c.view(torch.uint8)[page, :, slot].view(torch.float8_e4m3fn).double() * torch.exp2(power)[..., None]
 
     if op == "rope":
         return [turned(s["q"]), turned(s["k"])]
