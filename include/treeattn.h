@@ -70,7 +70,9 @@ typedef enum {
     TA_F32 = 0,
     TA_BF16 = 1,
     TA_I32 = 2,
-    TA_U64 = 3
+    TA_U64 = 3,
+    TA_E4M3 = 4,             /* 8-bit floating point, OCP e4m3: 448 is the largest value, 0x7f and 0xff are NaN */
+    TA_E8M0 = 5              /* a power of two, 2^(byte - 127); 255 is NaN */
 } ta_dtype;
 
 typedef enum {
@@ -325,6 +327,130 @@ int tree_attn_dispatch_row(int32_t index, int64_t row[8]);
 int tree_attn_fwd_static(const ta_tensor *q, const ta_tensor *k_cache, const ta_tensor *v_cache,
                          const ta_tensor *page_table, const ta_tensor *seq_lens, const ta_tensor *tree_parent,
                          ta_tensor *out, ta_tensor *lse, void *stream, const ta_opts *opts);
+
+/* ------------------------------------------------------------------------------------------------------------------
+ * Rotary positions.
+ *
+ * Pair j of a row's first R columns turns by angle position * freqs[j]: (a, b) -> amplitude * (a cos - b sin, b cos + a sin);
+ * columns R and up keep their values.  The angle is taken in 64 bits (at position 10^6 the 32-bit product is off by up to
+ * 0.03), the products in fp32, and the result is rounded once to the row's type.
+ */
+
+/* Rules for the frequencies (tree_attn_rope_freqs).  f_j = base^(-2j/R) is the plain rule; n_j = original * f_j / (2 pi) says
+ * how often pair j turns within the context the model was trained on. */
+#define TA_ROPE_PLAIN 0
+#define TA_ROPE_LINEAR 1      /* f_j / factor: positions drawn together */
+#define TA_ROPE_BANDS 2       /* f_j / factor where n_j < low, f_j where n_j > high, and between the two, linear in n_j */
+#define TA_ROPE_YARN 3        /* the same, and the amplitude is 0.1 ln(factor) + 1 (YaRN, Peng et al. 2023) */
+
+typedef struct {
+    int32_t rule;             /* TA_ROPE_* */
+    int32_t reserved;         /* must be 0 */
+    double base;              /* > 1 */
+    double factor;            /* >= 1; every rule but PLAIN */
+    double original;          /* > 0: tokens of the context the model was trained on; BANDS and YARN */
+    double low, high;         /* 0 <= low < high; BANDS and YARN */
+} ta_rope_rule;
+
+/* The frequencies of a model (host-only): freqs (HOST, rotary_dim / 2 floats) and, if given, the amplitude (HOST; 1 for every
+ * rule but YARN).  rotary_dim: R, even, 2 <= R <= TA_MAX_HEAD_DIM. */
+int tree_attn_rope_freqs(const ta_rope_rule *rule, int32_t rotary_dim, float *freqs, float *amplitude);
+
+typedef struct {
+    int32_t interleaved;      /* 0: column j is paired with j + R/2; 1: 2j with 2j + 1 */
+    float amplitude;          /* factor of the rotated columns, finite and >= 0; 0 = 1 */
+    const void *tree_masks;   /* optional DEVICE pointer, as in ta_opts: the ancestor masks of tree_parent's trees */
+    int64_t tree_masks_stride;
+    int32_t *status;          /* optional DEVICE pointer, as in ta_opts */
+} ta_rope_opts;
+
+/*
+ * Rotates the queries and keys of a step to their positions.
+ *
+ *   q, q_out     [B, T, Hq, D]  TA_BF16 or TA_F32, unit D stride.  q_out may be q itself (same pointer and strides), and must
+ *                not overlap it otherwise; no stride of an output may be 0 where its dimension is larger than 1.
+ *   k, k_out     [B, T, Hkv, D], the same; or both NULL.
+ *   freqs        TA_F32 [R/2], R <= D (tree_attn_rope_freqs, or any others)
+ *   seq_lens     TA_I32 [B], prefix lengths L_b
+ *   tree_parent  as in tree_attn_fwd (T <= TA_MAX_TREE): node i stands at position L_b + its depth (a root's is 0), which is
+ *                where its path lies when it is accepted.  NULL: token i stands at L_b + i, a chunk of a prompt of any length.
+ *
+ * A request with L_b < 0 or a malformed tree gets NaN rows, and its TA_STATUS_* bit is set.  NULL opts = defaults.
+ * One launch on `stream`, no allocation, no synchronisation.  B == 0 is a no-op.
+ */
+int tree_attn_rope(const ta_tensor *q, const ta_tensor *k, const ta_tensor *freqs, const ta_tensor *seq_lens,
+                   const ta_tensor *tree_parent, ta_tensor *q_out, ta_tensor *k_out, void *stream, const ta_rope_opts *opts);
+
+/* ------------------------------------------------------------------------------------------------------------------
+ * The 8-bit cache.
+ *
+ *   k_cache, v_cache   TA_E4M3 [num_pages, Hkv, page_size, D], any 4-D strided view with unit D stride
+ *   k_scale, v_scale   TA_E8M0 [num_pages, Hkv, page_size], any strides
+ *
+ * The value of column d is code[d] * scale, one scale per token and KV head: D + 1 bytes a row instead of 2 D.  Paging is that of
+ * tree_attn_fwd (page_table NULL = contiguous).  A row is written with the smallest scale 2^e, e >= -126, that leaves its largest
+ * finite magnitude at 448 or less (1 for a row of zeros); every value is then rounded to the nearest code, ties to even, so that it is
+ * off by at most 2^-4 of itself down to 2^-6 * scale, and below by at most 2^-10 * scale.  A NaN or an infinity becomes a NaN code.
+ */
+
+/*
+ * Quantising write-back: k_new, v_new [B, T, Hkv, D] (TA_BF16 or TA_F32, unit D stride) go to logical positions L_b .. L_b+T-1,
+ * as in tree_attn_append, but T may be any number of tokens that the page table can hold: a step's tree or a prompt.  A request
+ * with L_b < 0 or L_b + T beyond its page table is skipped (TA_STATUS_BAD_SEQLEN), so is a token whose page lies outside the
+ * cache (TA_STATUS_BAD_PAGE).  One launch on `stream`, no allocation, no synchronisation.
+ */
+int tree_attn_q8_append(const ta_tensor *k_new, const ta_tensor *v_new, ta_tensor *k_cache, ta_tensor *v_cache,
+                        ta_tensor *k_scale, ta_tensor *v_scale, const ta_tensor *page_table, const ta_tensor *seq_lens,
+                        void *stream);
+
+/*
+ * tree_attn_rope of q and k_new, and tree_attn_q8_append of the rotated keys and v_new, in one launch that does not write the
+ * rotated keys anywhere else: bit for bit what the two calls give (the keys are rounded to their type in between).  q and k_new
+ * are not changed (q_out may be q).  A request with a bad length or tree gets NaN rows of q_out and is not written.
+ */
+int tree_attn_q8_rope_append(const ta_tensor *q, const ta_tensor *k_new, const ta_tensor *v_new, const ta_tensor *freqs,
+                             const ta_tensor *seq_lens, const ta_tensor *tree_parent, ta_tensor *q_out, ta_tensor *k_cache,
+                             ta_tensor *v_cache, ta_tensor *k_scale, ta_tensor *v_scale, const ta_tensor *page_table,
+                             void *stream, const ta_rope_opts *opts);
+
+/*
+ * Reads a part of the cache back: rows i < counts[b] of k_out, v_out [B, N, Hkv, D] (TA_BF16 or TA_F32, unit D stride, rounded
+ * once) receive logical positions starts[b] + i; rows from counts[b] on are left as they are.
+ *
+ *   starts   TA_I32 [B], or NULL = 0
+ *   counts   TA_I32 [B], 0 <= counts[b] <= N
+ *
+ * A request with a negative start, a count outside [0, N] or an end beyond its page table gets NaN in all its N rows
+ * (TA_STATUS_BAD_SEQLEN); rows on a page outside the cache are NaN (TA_STATUS_BAD_PAGE).  One launch, no allocation.
+ */
+int tree_attn_q8_read(const ta_tensor *k_cache, const ta_tensor *v_cache, const ta_tensor *k_scale, const ta_tensor *v_scale,
+                      const ta_tensor *page_table, const ta_tensor *starts, const ta_tensor *counts, ta_tensor *k_out,
+                      ta_tensor *v_out, void *stream);
+
+/* tree_attn_compact for the 8-bit cache: codes and scales of the accepted path move together, unchanged. */
+int tree_attn_q8_compact(ta_tensor *k_cache, ta_tensor *v_cache, ta_tensor *k_scale, ta_tensor *v_scale,
+                         const ta_tensor *page_table, const ta_tensor *seq_lens, const ta_tensor *accepted,
+                         const ta_tensor *n_accepted, int32_t tree_size, ta_tensor *seq_lens_out, void *stream);
+
+/*
+ * tree_attn_fwd_ex over the 8-bit cache, for one new token or a tree of them: q and out TA_BF16 or TA_F32, everything else, the
+ * workspace and the errors as there.  Scores and outputs are those of the values code * scale, which are used as they are:
+ * q is not rounded, bf16 probabilities are (fp32 ones not).  opts: k_new and v_new must be NULL (TA_ERR_OPTS; tree_attn_q8_append
+ * writes the tree tokens); kernel TA_KERNEL_GENERIC names the scalar kernel, TA_KERNEL_MFMA (or _BASIC) the matrix-core one, which
+ * takes head_dim 64 or 128, power-of-two pages or contiguous, 16-byte aligned q, K and V rows, and at most 256 query heads per
+ * KV head.
+ * A NaN among the codes or scales that a row attends to makes it NaN; one that it does not attend to changes nothing.
+ */
+int tree_attn_q8_fwd(const ta_tensor *q, const ta_tensor *k_cache, const ta_tensor *v_cache, const ta_tensor *k_scale,
+                     const ta_tensor *v_scale, const ta_tensor *page_table, const ta_tensor *seq_lens,
+                     const ta_tensor *tree_parent, ta_tensor *out, ta_tensor *lse, void *stream, const ta_opts *opts);
+
+/* The launch plan of such a call (host-only): tree_attn_plan's figures; plan[11], the table row, is -1.  plan[12] is the workspace
+ * it needs, for tree_attn_reserve or ta_opts.workspace (tree_attn_workspace_bytes does not speak of this call). */
+int tree_attn_q8_plan(const ta_tensor *q, const ta_tensor *k_cache, const ta_tensor *v_cache, const ta_tensor *k_scale,
+                      const ta_tensor *v_scale, const ta_tensor *page_table, const ta_tensor *seq_lens,
+                      const ta_tensor *tree_parent, const ta_tensor *out, const ta_tensor *lse, const ta_opts *opts,
+                      int32_t num_cus, int64_t plan[16]);
 
 /*
  * Measurement aid (no part of the method): a plain streaming read of `bytes` bytes of device memory at `buf`

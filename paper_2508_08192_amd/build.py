@@ -9,7 +9,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtreeattn.so")
-SOURCES = ["ta_api.hip", "ta_generic.hip", "ta_mfma.hip", "ta_mfma_ks.hip", "ta_f32.hip", "ta_host.cpp"]
+SOURCES = ["ta_api.hip", "ta_generic.hip", "ta_mfma.hip", "ta_mfma_ks.hip", "ta_f32.hip", "ta_q8.hip", "ta_host.cpp",
+           "ta_q8_host.cpp"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
     # hipcc must not form packed-fp32 instructions on these machines
@@ -101,7 +102,8 @@ def build_host_checked(verbose=False):
     tmp = HOST_CHECKED_LIB + ".tmp%d" % os.getpid()
     cmd = [gxx, "-std=c++17", "-O1", "-g", "-fPIC", "-shared", "-Wall", "-Wextra", "-Werror",
            "-fsanitize=address,undefined", "-fno-sanitize-recover=all", "-fno-omit-frame-pointer",
-           os.path.join(CSRC, "ta_host.cpp"), os.path.join(CSRC, "ta_host_only.cpp"), "-o", tmp]
+           os.path.join(CSRC, "ta_host.cpp"), os.path.join(CSRC, "ta_q8_host.cpp"), os.path.join(CSRC, "ta_host_only.cpp"),
+           "-o", tmp]
     if verbose:
         print(" ".join(cmd), flush=True)
     proc = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)

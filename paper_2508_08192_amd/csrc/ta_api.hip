@@ -4,7 +4,7 @@
 #include <mutex>
 #include <vector>
 
-#include "ta_common.h"
+#include "ta_q8.h"
 
 namespace {
 
@@ -100,6 +100,39 @@ void place_workspace(TAProblem &pr, void *ws)
     pr.p.ws_parts = (int32_t *)((char *)ws + pr.ws_o_bytes + pr.ws_lse_bytes);
 }
 
+// The library-owned workspace for a call on `st`, grown if need be.
+int owned_workspace(DeviceState *s, hipStream_t st, TAProblem &pr)
+{
+    std::lock_guard<std::mutex> lk(s->ws_mu);
+    if (pr.ws_bytes > s->ws_bytes) {
+        // growing means hipMalloc, which stream capture forbids: such a caller reserves beforehand
+        hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+        if (hipStreamIsCapturing(st, &cap) != hipSuccess) {
+            (void)hipGetLastError();
+            return TA_ERR_HIP;
+        }
+        if (cap != hipStreamCaptureStatusNone)
+            return TA_ERR_WORKSPACE;
+        const int rc = reserve_locked(s, pr.ws_bytes);
+        if (rc != TA_OK)
+            return rc;
+    }
+    place_workspace(pr, s->ws);
+    return TA_OK;
+}
+
+int launch_rows_call(TARows &r, void *stream)
+{
+    if (r.B == 0)
+        return TA_OK;
+    DeviceState *s = nullptr;
+    const int rc = device_state(&s);
+    if (rc != TA_OK)
+        return rc;
+    r.status = s->status;
+    return ta_launch_rows(r, (hipStream_t)stream) == hipSuccess ? TA_OK : TA_ERR_HIP;
+}
+
 // KV pass and merge pass of a planned call on `stream`.
 int launch_call(const TAProblem &pr, hipStream_t st, int dev, void *const *ev)
 {
@@ -183,21 +216,9 @@ int tree_attn_fwd_ex(const ta_tensor *q, const ta_tensor *k_cache, const ta_tens
         return rc;
     hipStream_t st = (hipStream_t)stream;
     if (!pr.p.ws_o) {
-        std::lock_guard<std::mutex> lk(s->ws_mu);
-        if (pr.ws_bytes > s->ws_bytes) {
-            // growing means hipMalloc, which stream capture forbids: such a caller reserves beforehand
-            hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
-            if (hipStreamIsCapturing(st, &cap) != hipSuccess) {
-                (void)hipGetLastError();
-                return TA_ERR_HIP;
-            }
-            if (cap != hipStreamCaptureStatusNone)
-                return TA_ERR_WORKSPACE;
-            rc = reserve_locked(s, pr.ws_bytes);
-            if (rc != TA_OK)
-                return rc;
-        }
-        place_workspace(pr, s->ws);
+        rc = owned_workspace(s, st, pr);
+        if (rc != TA_OK)
+            return rc;
     }
     pr.p.status = s->status;
     return launch_call(pr, st, dev, opts ? opts->events : nullptr);
@@ -285,6 +306,103 @@ int tree_attn_compact(ta_tensor *k_cache, ta_tensor *v_cache, const ta_tensor *p
         return rc;
     c.status = s->status;
     return ta_launch_compact(c, (hipStream_t)stream) == hipSuccess ? TA_OK : TA_ERR_HIP;
+}
+
+int tree_attn_rope(const ta_tensor *q, const ta_tensor *k, const ta_tensor *freqs, const ta_tensor *seq_lens,
+                   const ta_tensor *tree_parent, ta_tensor *q_out, ta_tensor *k_out, void *stream, const ta_rope_opts *opts)
+{
+    TARows r;
+    const int rc = ta_host_check_rope(q, k, freqs, seq_lens, tree_parent, q_out, k_out, opts, &r);
+    return rc != TA_OK ? rc : launch_rows_call(r, stream);
+}
+
+int tree_attn_q8_append(const ta_tensor *k_new, const ta_tensor *v_new, ta_tensor *k_cache, ta_tensor *v_cache,
+                        ta_tensor *k_scale, ta_tensor *v_scale, const ta_tensor *page_table, const ta_tensor *seq_lens,
+                        void *stream)
+{
+    TARows r;
+    const int rc = ta_host_check_q8_append(k_new, v_new, k_cache, v_cache, k_scale, v_scale, page_table, seq_lens, &r);
+    return rc != TA_OK ? rc : launch_rows_call(r, stream);
+}
+
+int tree_attn_q8_rope_append(const ta_tensor *q, const ta_tensor *k_new, const ta_tensor *v_new, const ta_tensor *freqs,
+                             const ta_tensor *seq_lens, const ta_tensor *tree_parent, ta_tensor *q_out, ta_tensor *k_cache,
+                             ta_tensor *v_cache, ta_tensor *k_scale, ta_tensor *v_scale, const ta_tensor *page_table,
+                             void *stream, const ta_rope_opts *opts)
+{
+    TARows r;
+    const int rc = ta_host_check_q8_rope_append(q, k_new, v_new, freqs, seq_lens, tree_parent, q_out, k_cache, v_cache, k_scale,
+                                                v_scale, page_table, opts, &r);
+    return rc != TA_OK ? rc : launch_rows_call(r, stream);
+}
+
+int tree_attn_q8_read(const ta_tensor *k_cache, const ta_tensor *v_cache, const ta_tensor *k_scale, const ta_tensor *v_scale,
+                      const ta_tensor *page_table, const ta_tensor *starts, const ta_tensor *counts, ta_tensor *k_out,
+                      ta_tensor *v_out, void *stream)
+{
+    TAQ8Read r;
+    int rc = ta_host_check_q8_read(k_cache, v_cache, k_scale, v_scale, page_table, starts, counts, k_out, v_out, &r);
+    if (rc != TA_OK || r.B == 0 || r.N == 0)
+        return rc;
+    DeviceState *s = nullptr;
+    rc = device_state(&s);
+    if (rc != TA_OK)
+        return rc;
+    r.status = s->status;
+    return ta_launch_q8_read(r, (hipStream_t)stream) == hipSuccess ? TA_OK : TA_ERR_HIP;
+}
+
+int tree_attn_q8_compact(ta_tensor *k_cache, ta_tensor *v_cache, ta_tensor *k_scale, ta_tensor *v_scale,
+                         const ta_tensor *page_table, const ta_tensor *seq_lens, const ta_tensor *accepted,
+                         const ta_tensor *n_accepted, int32_t tree_size, ta_tensor *seq_lens_out, void *stream)
+{
+    TAQ8Compact c;
+    int rc = ta_host_check_q8_compact(k_cache, v_cache, k_scale, v_scale, page_table, seq_lens, accepted, n_accepted, tree_size,
+                                      seq_lens_out, &c);
+    if (rc != TA_OK || c.B == 0)
+        return rc;
+    DeviceState *s = nullptr;
+    rc = device_state(&s);
+    if (rc != TA_OK)
+        return rc;
+    c.status = s->status;
+    return ta_launch_q8_compact(c, (hipStream_t)stream) == hipSuccess ? TA_OK : TA_ERR_HIP;
+}
+
+int tree_attn_q8_fwd(const ta_tensor *q, const ta_tensor *k_cache, const ta_tensor *v_cache, const ta_tensor *k_scale,
+                     const ta_tensor *v_scale, const ta_tensor *page_table, const ta_tensor *seq_lens,
+                     const ta_tensor *tree_parent, ta_tensor *out, ta_tensor *lse, void *stream, const ta_opts *opts)
+{
+    TAQ8Problem qp;
+    TAProblem &pr = qp.pr;
+    // (a nominal CU count first: host-visible errors are reported before any HIP call)
+    int rc = ta_host_build_q8_problem(q, k_cache, v_cache, k_scale, v_scale, page_table, seq_lens, tree_parent, out, lse, opts, 256,
+                                      &qp);
+    if (rc != TA_OK || pr.p.B == 0)
+        return rc;
+    DeviceState *s = nullptr;
+    int dev = 0;
+    rc = device_state(&s, &dev);
+    if (rc != TA_OK)
+        return rc;
+    if (s->num_cus != 256)
+        rc = ta_host_build_q8_problem(q, k_cache, v_cache, k_scale, v_scale, page_table, seq_lens, tree_parent, out, lse, opts,
+                                      s->num_cus, &qp);
+    if (rc != TA_OK)
+        return rc;
+    hipStream_t st = (hipStream_t)stream;
+    if (!pr.p.ws_o) {
+        rc = owned_workspace(s, st, pr);
+        if (rc != TA_OK)
+            return rc;
+    }
+    pr.p.status = s->status;
+    const TAQ8Params &p = ta_host_q8_params(&qp);
+    void *const *ev = opts ? opts->events : nullptr;
+    auto mark = [&](int i) { return !ev || !ev[i] || hipEventRecord((hipEvent_t)ev[i], st) == hipSuccess; };
+    if (!mark(0) || ta_launch_q8_generic(p, st, dev) != hipSuccess || !mark(1) || ta_launch_merge(p, st) != hipSuccess || !mark(2))
+        return TA_ERR_HIP;
+    return TA_OK;
 }
 
 int tree_attn_last_status(int32_t *host_status, void *stream)

@@ -135,38 +135,46 @@ PyObject *py_fwd(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     return PyLong_FromLong(rc);
 }
 
+// Scale, split, kernel, item cost, masks, window starts and node offset of a call, in this order, into options.
+bool read_opts(PyObject *const *args, ta_opts *o)
+{
+    memset(o, 0, sizeof *o);
+    ta_tensor dm;
+    if (args[0] != Py_None) {
+        if (!PyFloat_CheckExact(args[0]))
+            return false;
+        o->scale = (float)PyFloat_AS_DOUBLE(args[0]);
+    }
+    if (!read_int32(args[1], &o->num_splits) || !read_int32(args[2], &o->kernel) || !read_int32(args[3], &o->item_cost) ||
+        !read_int32(args[6], &o->q_node_offset))
+        return false;
+    if (args[4] != Py_None) {
+        if (!describe(args[4], &dm))
+            return false;
+        o->tree_masks = dm.data;
+        o->tree_masks_stride = dm.ndim == 2 ? dm.stride[0] : 0;
+    }
+    if (args[5] != Py_None) {
+        void *at;
+        if (!is_plain(args[5]) || !read_ptr(args[5], &at))
+            return false;
+        o->kv_start = at;
+    }
+    return true;
+}
+
 // fwd_ex(entry, stream, the eight tensors, scale, num_splits, kernel, item_cost, tree_masks, kv_start, q_node_offset, k_new,
 // v_new) -> status or None (entry: tree_attn_fwd_ex or tree_attn_fwd_static)
 PyObject *py_fwd_ex(PyObject *, PyObject *const *args, Py_ssize_t nargs)
 {
     typedef int (*fn_t)(const ta_tensor *, const ta_tensor *, const ta_tensor *, const ta_tensor *, const ta_tensor *,
                         const ta_tensor *, ta_tensor *, ta_tensor *, void *, const ta_opts *);
-    ta_tensor d[8], *t[8], dn[2], *tn[2], dm;
+    ta_tensor d[8], *t[8], dn[2], *tn[2];
     ta_opts o;
-    void *fn, *stream, *at;
-    if (nargs != 19 || !read_address(args[0], &fn) || !read_address(args[1], &stream) || !describe_all(args + 2, 8, d, t))
+    void *fn, *stream;
+    if (nargs != 19 || !read_address(args[0], &fn) || !read_address(args[1], &stream) || !describe_all(args + 2, 8, d, t) ||
+        !read_opts(args + 10, &o))
         return elsewhere();
-    memset(&o, 0, sizeof o);
-    PyObject *scale = args[10], *masks = args[14], *starts = args[15];
-    if (scale != Py_None) {
-        if (!PyFloat_CheckExact(scale))
-            return elsewhere();
-        o.scale = (float)PyFloat_AS_DOUBLE(scale);
-    }
-    if (!read_int32(args[11], &o.num_splits) || !read_int32(args[12], &o.kernel) || !read_int32(args[13], &o.item_cost) ||
-        !read_int32(args[16], &o.q_node_offset))
-        return elsewhere();
-    if (masks != Py_None) {
-        if (!describe(masks, &dm))
-            return elsewhere();
-        o.tree_masks = dm.data;
-        o.tree_masks_stride = dm.ndim == 2 ? dm.stride[0] : 0;
-    }
-    if (starts != Py_None) {
-        if (!is_plain(starts) || !read_ptr(starts, &at))
-            return elsewhere();
-        o.kv_start = at;
-    }
     if (!describe_all(args + 17, 2, dn, tn))
         return elsewhere();
     o.k_new = tn[0];
@@ -213,6 +221,98 @@ PyObject *py_compact(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     return PyLong_FromLong(rc);
 }
 
+typedef const ta_tensor *ct;
+
+// plain(entry, stream, eight or nine tensors) -> status or None: calls that take tensors and the stream
+PyObject *py_plain(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    typedef int (*fn8_t)(ct, ct, ct, ct, ct, ct, ct, ct, void *);
+    typedef int (*fn9_t)(ct, ct, ct, ct, ct, ct, ct, ct, ct, void *);
+    ta_tensor d[9], *t[9];
+    void *fn, *stream;
+    if ((nargs != 10 && nargs != 11) || !read_address(args[0], &fn) || !read_address(args[1], &stream) ||
+        !describe_all(args + 2, (int)nargs - 2, d, t))
+        return elsewhere();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    if (nargs == 10)
+        rc = ((fn8_t)fn)(t[0], t[1], t[2], t[3], t[4], t[5], t[6], t[7], stream);
+    else
+        rc = ((fn9_t)fn)(t[0], t[1], t[2], t[3], t[4], t[5], t[6], t[7], t[8], stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+// turn(entry, stream, interleaved, amplitude, tree_masks, seven or twelve tensors) -> status or None
+PyObject *py_turn(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    typedef int (*fn7_t)(ct, ct, ct, ct, ct, ct, ct, void *, const ta_rope_opts *);
+    typedef int (*fn12_t)(ct, ct, ct, ct, ct, ct, ct, ct, ct, ct, ct, ct, void *, const ta_rope_opts *);
+    ta_tensor d[12], *t[12], dm;
+    ta_rope_opts o;
+    void *fn, *stream;
+    memset(&o, 0, sizeof o);
+    if ((nargs != 12 && nargs != 17) || !read_address(args[0], &fn) || !read_address(args[1], &stream) ||
+        !PyBool_Check(args[2]) || !describe_all(args + 5, (int)nargs - 5, d, t))
+        return elsewhere();
+    o.interleaved = args[2] == Py_True;
+    if (args[3] != Py_None) {
+        if (!PyFloat_CheckExact(args[3]))
+            return elsewhere();
+        o.amplitude = (float)PyFloat_AS_DOUBLE(args[3]);
+    }
+    if (args[4] != Py_None) {
+        if (!describe(args[4], &dm))
+            return elsewhere();
+        o.tree_masks = dm.data;
+        o.tree_masks_stride = dm.ndim == 2 ? dm.stride[0] : 0;
+    }
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    if (nargs == 12)
+        rc = ((fn7_t)fn)(t[0], t[1], t[2], t[3], t[4], t[5], t[6], stream, &o);
+    else
+        rc = ((fn12_t)fn)(t[0], t[1], t[2], t[3], t[4], t[5], t[6], t[7], t[8], t[9], t[10], t[11], stream, &o);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+// q8_compact(entry, stream, k_cache, v_cache, k_scale, v_scale, page_table, seq_lens, accepted, n_accepted, seq_lens_out,
+// tree_size) -> status or None
+PyObject *py_q8_compact(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    typedef int (*fn_t)(ct, ct, ct, ct, ct, ct, ct, ct, int32_t, ct, void *);
+    ta_tensor d[9], *t[9];
+    void *fn, *stream;
+    int32_t tree_size;
+    if (nargs != 12 || !read_address(args[0], &fn) || !read_address(args[1], &stream) || !describe_all(args + 2, 9, d, t) ||
+        !read_int32(args[11], &tree_size))
+        return elsewhere();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = ((fn_t)fn)(t[0], t[1], t[2], t[3], t[4], t[5], t[6], t[7], tree_size, t[8], stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+// q8_fwd(entry, stream, q, k_cache, v_cache, k_scale, v_scale, page_table, seq_lens, tree_parent, out, lse, scale, num_splits,
+// kernel, item_cost, tree_masks, kv_start, q_node_offset) -> status or None
+PyObject *py_q8_fwd(PyObject *, PyObject *const *args, Py_ssize_t nargs)
+{
+    typedef int (*fn_t)(ct, ct, ct, ct, ct, ct, ct, ct, ct, ct, void *, const ta_opts *);
+    ta_tensor d[10], *t[10];
+    ta_opts o;
+    void *fn, *stream;
+    if (nargs != 19 || !read_address(args[0], &fn) || !read_address(args[1], &stream) || !describe_all(args + 2, 10, d, t) ||
+        !read_opts(args + 12, &o))
+        return elsewhere();
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = ((fn_t)fn)(t[0], t[1], t[2], t[3], t[4], t[5], t[6], t[7], t[8], t[9], stream, &o);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
 // setup(Tensor, Parameter, ((dtype, code), ...)): the types and element types that describe() knows.  Called once.
 PyObject *py_setup(PyObject *, PyObject *args)
 {
@@ -242,6 +342,10 @@ PyMethodDef kMethods[] = {
     {"fwd_ex", (PyCFunction)(void (*)(void))py_fwd_ex, METH_FASTCALL, nullptr},
     {"append", (PyCFunction)(void (*)(void))py_append, METH_FASTCALL, nullptr},
     {"compact", (PyCFunction)(void (*)(void))py_compact, METH_FASTCALL, nullptr},
+    {"plain", (PyCFunction)(void (*)(void))py_plain, METH_FASTCALL, nullptr},
+    {"turn", (PyCFunction)(void (*)(void))py_turn, METH_FASTCALL, nullptr},
+    {"q8_compact", (PyCFunction)(void (*)(void))py_q8_compact, METH_FASTCALL, nullptr},
+    {"q8_fwd", (PyCFunction)(void (*)(void))py_q8_fwd, METH_FASTCALL, nullptr},
     {"setup", py_setup, METH_VARARGS, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };

@@ -4,7 +4,7 @@
 // ta_mfma.hip, ta_mfma_ks.hip and ta_f32.hip and share the schedule and the merge.
 #include <type_traits>
 
-#include "ta_common.h"
+#include "ta_q8.h"
 
 #define GEN_THREADS 256
 #define GEN_WAVES (GEN_THREADS / TA_WAVE)
@@ -49,12 +49,14 @@ __device__ __forceinline__ void gen_lds_barrier()
 // updates its rows -- lanes are the tile's tokens for the scores, then head-dim columns for the weighted sum
 // of V.  Running max / sum per row (base-2 domain).  Tokens that do not exist are staged as zeros.
 // DCH = 64-column chunks of the head dimension a lane carries (1, 2 or 4).  A wave carries RB query rows at a time
+// Args: TAParams, or TAQ8Params for the 8-bit cache, whose codes become fp32 values as they are staged.
 // (eight with one chunk, which halves the passes over the tile list of the small-head shapes) and stages sixteen
 // tokens of every tile; their loads go out one tile ahead, so that a tile's global round trip runs under the
 // arithmetic of the tile before it, and Q's under the first tile's.
-template <bool BF16, int DCH>
-__global__ __launch_bounds__(GEN_THREADS) void ta_generic_kv_kernel(TA_SCHED_PARAMS, TAParams p)
+template <bool BF16, int DCH, typename Args>
+__global__ __launch_bounds__(GEN_THREADS) void ta_generic_kv_kernel(TA_SCHED_PARAMS, Args p)
 {
+    constexpr bool Q8 = std::is_same<Args, TAQ8Params>::value;
     constexpr int RB = DCH == 1 ? 8 : 4;
     extern __shared__ int smem_i[];
     int *cum = smem_i;                                                   // [B + 1]
@@ -182,6 +184,7 @@ __global__ __launch_bounds__(GEN_THREADS) void ta_generic_kv_kernel(TA_SCHED_PAR
             // while the tile before is computed.  Tokens that do not exist are staged as zeros.
             constexpr int TOK = TA_TILE / GEN_WAVES;
             uint32_t kbits[TOK][DCH], vbits[TOK][DCH];
+            uint32_t kscale[Q8 ? TOK : 1], vscale[Q8 ? TOK : 1];
             auto load_tile = [&](int j) {
                 const bool tree_tile = (j == n_b - 1);
 #pragma unroll
@@ -200,12 +203,22 @@ __global__ __launch_bounds__(GEN_THREADS) void ta_generic_kv_kernel(TA_SCHED_PAR
                         koff = ta_cache_offset(p, b, g, pos, p.k_sp, p.k_sh, p.k_ss);
                         voff = ta_cache_offset(p, b, g, pos, p.v_sp, p.v_sh, p.v_ss);
                     }
+                    if constexpr (Q8) {
+                        const bool there = exists && koff >= 0 && voff >= 0;
+                        kscale[u] = there ? p.ks[ta_cache_offset(p, b, g, pos, p.ks_sp, p.ks_sh, p.ks_ss)] : 127u;
+                        vscale[u] = there ? p.vs[ta_cache_offset(p, b, g, pos, p.vs_sp, p.vs_sh, p.vs_ss)] : 127u;
+                    }
 #pragma unroll
                     for (int c = 0; c < DCH; ++c) {
                         const int d = lane + c * TA_WAVE;
                         const bool ld = exists && d < p.D && koff >= 0 && voff >= 0;
-                        kbits[u][c] = ld ? load_bits<BF16>(kb, koff, (uint32_t)d) : 0u;
-                        vbits[u][c] = ld ? load_bits<BF16>(vb, voff, (uint32_t)d) : 0u;
+                        if constexpr (Q8) {
+                            kbits[u][c] = ld ? ((const uint8_t *)kb + koff)[d] : 0u;
+                            vbits[u][c] = ld ? ((const uint8_t *)vb + voff)[d] : 0u;
+                        } else {
+                            kbits[u][c] = ld ? load_bits<BF16>(kb, koff, (uint32_t)d) : 0u;
+                            vbits[u][c] = ld ? load_bits<BF16>(vb, voff, (uint32_t)d) : 0u;
+                        }
                     }
                 }
             };
@@ -219,8 +232,13 @@ __global__ __launch_bounds__(GEN_THREADS) void ta_generic_kv_kernel(TA_SCHED_PAR
                     for (int c = 0; c < DCH; ++c) {
                         const int d = lane + c * TA_WAVE;
                         if (d < p.D) {
-                            kt[(wave * TOK + u) * ldk + d] = bits_value<BF16>(kbits[u][c]);
-                            vt[(wave * TOK + u) * p.D + d] = bits_value<BF16>(vbits[u][c]);
+                            if constexpr (Q8) {
+                                kt[(wave * TOK + u) * ldk + d] = q8_value(kbits[u][c]) * q8_scale(kscale[u]);
+                                vt[(wave * TOK + u) * p.D + d] = q8_value(vbits[u][c]) * q8_scale(vscale[u]);
+                            } else {
+                                kt[(wave * TOK + u) * ldk + d] = bits_value<BF16>(kbits[u][c]);
+                                vt[(wave * TOK + u) * p.D + d] = bits_value<BF16>(vbits[u][c]);
+                            }
                         }
                     }
                 if (j == j0) {
@@ -284,6 +302,10 @@ __global__ __launch_bounds__(GEN_THREADS) void ta_generic_kv_kernel(TA_SCHED_PAR
 #pragma unroll
                     for (int i = 0; i < RB; ++i) {
                         const float pj = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(pr[i]), jj));  // scalar
+                        if constexpr (Q8) {                // a NaN of a node that is no ancestor counts for nothing
+                            if (tree_tile && !((mask[i] >> jj) & 1ull))
+                                continue;
+                        }
 #pragma unroll
                         for (int c = 0; c < DCH; ++c)
                             acc[i][c] = fmaf(pj, vj[c], acc[i][c]);
@@ -311,8 +333,8 @@ __global__ __launch_bounds__(GEN_THREADS) void ta_generic_kv_kernel(TA_SCHED_PAR
     }
 }
 
-template <bool BF16, int DCH>
-static hipError_t launch_generic_instance(const TAParams &p, hipStream_t stream, bool *attr_done)
+template <bool BF16, int DCH, typename Args>
+static hipError_t launch_generic_instance(const Args &p, hipStream_t stream, bool *attr_done)
 {
     constexpr int RB = DCH == 1 ? 8 : 4;
     const size_t smem = sizeof(int) * (((p.B + 2) & ~1) + 2 * ((p.B + 1) & ~1)) + sizeof(unsigned long long) * TA_MAX_TREE + 16 +
@@ -321,31 +343,35 @@ static hipError_t launch_generic_instance(const TAParams &p, hipStream_t stream,
     if (smem > 160 * 1024 - 512)
         return hipErrorInvalidValue;
     if (!*attr_done) {
-        hipError_t e = hipFuncSetAttribute((const void *)ta_generic_kv_kernel<BF16, DCH>,
+        hipError_t e = hipFuncSetAttribute((const void *)ta_generic_kv_kernel<BF16, DCH, Args>,
                                            hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024 - 512);
         if (e != hipSuccess)
             return e;
         *attr_done = true;
     }
-    hipLaunchKernelGGL((ta_generic_kv_kernel<BF16, DCH>), dim3(p.n_wg, p.n_rg), dim3(GEN_THREADS), smem, stream, TA_SCHED_ARGS(p), p);
+    hipLaunchKernelGGL((ta_generic_kv_kernel<BF16, DCH, Args>), dim3(p.n_wg, p.n_rg), dim3(GEN_THREADS), smem, stream, TA_SCHED_ARGS(p), p);
     return hipGetLastError();
 }
 
-hipError_t ta_launch_generic(const TAParams &p, hipStream_t stream, int dev)
+template <typename Args>
+static hipError_t launch_generic(const Args &p, hipStream_t stream, int dev)
 {
     static bool attr_set[64][2][3] = {};
     if (dev < 0 || dev >= 64)
         return hipErrorInvalidDevice;
     const int bf = p.is_bf16 ? 1 : 0;
     if (p.D <= TA_WAVE)
-        return bf ? launch_generic_instance<true, 1>(p, stream, &attr_set[dev][1][0])
-                  : launch_generic_instance<false, 1>(p, stream, &attr_set[dev][0][0]);
+        return bf ? launch_generic_instance<true, 1, Args>(p, stream, &attr_set[dev][1][0])
+                  : launch_generic_instance<false, 1, Args>(p, stream, &attr_set[dev][0][0]);
     if (p.D <= 2 * TA_WAVE)
-        return bf ? launch_generic_instance<true, 2>(p, stream, &attr_set[dev][1][1])
-                  : launch_generic_instance<false, 2>(p, stream, &attr_set[dev][0][1]);
-    return bf ? launch_generic_instance<true, 4>(p, stream, &attr_set[dev][1][2])
-              : launch_generic_instance<false, 4>(p, stream, &attr_set[dev][0][2]);
+        return bf ? launch_generic_instance<true, 2, Args>(p, stream, &attr_set[dev][1][1])
+                  : launch_generic_instance<false, 2, Args>(p, stream, &attr_set[dev][0][1]);
+    return bf ? launch_generic_instance<true, 4, Args>(p, stream, &attr_set[dev][1][2])
+              : launch_generic_instance<false, 4, Args>(p, stream, &attr_set[dev][0][2]);
 }
+
+hipError_t ta_launch_generic(const TAParams &p, hipStream_t stream, int dev) { return launch_generic(p, stream, dev); }
+hipError_t ta_launch_q8_generic(const TAQ8Params &p, hipStream_t stream, int dev) { return launch_generic(p, stream, dev); }
 
 // Merge pass (section 3.1: full attention from partial attentions over disjoint chunks of the keys,
 // through their log-sum-exps).  One wave per output row: lanes first span the partials of the row

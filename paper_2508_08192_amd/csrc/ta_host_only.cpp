@@ -76,6 +76,62 @@ int tree_attn_compact(ta_tensor *k_cache, ta_tensor *v_cache, const ta_tensor *p
     return rc != TA_OK || c.B == 0 ? rc : TA_ERR_HIP;
 }
 
+int tree_attn_rope(const ta_tensor *q, const ta_tensor *k, const ta_tensor *freqs, const ta_tensor *seq_lens,
+                   const ta_tensor *tree_parent, ta_tensor *q_out, ta_tensor *k_out, void *, const ta_rope_opts *opts)
+{
+    TARows r;
+    const int rc = ta_host_check_rope(q, k, freqs, seq_lens, tree_parent, q_out, k_out, opts, &r);
+    return rc != TA_OK || r.B == 0 ? rc : TA_ERR_HIP;
+}
+
+int tree_attn_q8_append(const ta_tensor *k_new, const ta_tensor *v_new, ta_tensor *k_cache, ta_tensor *v_cache,
+                        ta_tensor *k_scale, ta_tensor *v_scale, const ta_tensor *page_table, const ta_tensor *seq_lens, void *)
+{
+    TARows r;
+    const int rc = ta_host_check_q8_append(k_new, v_new, k_cache, v_cache, k_scale, v_scale, page_table, seq_lens, &r);
+    return rc != TA_OK || r.B == 0 ? rc : TA_ERR_HIP;
+}
+
+int tree_attn_q8_rope_append(const ta_tensor *q, const ta_tensor *k_new, const ta_tensor *v_new, const ta_tensor *freqs,
+                             const ta_tensor *seq_lens, const ta_tensor *tree_parent, ta_tensor *q_out, ta_tensor *k_cache,
+                             ta_tensor *v_cache, ta_tensor *k_scale, ta_tensor *v_scale, const ta_tensor *page_table, void *,
+                             const ta_rope_opts *opts)
+{
+    TARows r;
+    const int rc = ta_host_check_q8_rope_append(q, k_new, v_new, freqs, seq_lens, tree_parent, q_out, k_cache, v_cache, k_scale,
+                                                v_scale, page_table, opts, &r);
+    return rc != TA_OK || r.B == 0 ? rc : TA_ERR_HIP;
+}
+
+int tree_attn_q8_read(const ta_tensor *k_cache, const ta_tensor *v_cache, const ta_tensor *k_scale, const ta_tensor *v_scale,
+                      const ta_tensor *page_table, const ta_tensor *starts, const ta_tensor *counts, ta_tensor *k_out,
+                      ta_tensor *v_out, void *)
+{
+    TAQ8Read r;
+    const int rc = ta_host_check_q8_read(k_cache, v_cache, k_scale, v_scale, page_table, starts, counts, k_out, v_out, &r);
+    return rc != TA_OK || r.B == 0 || r.N == 0 ? rc : TA_ERR_HIP;
+}
+
+int tree_attn_q8_compact(ta_tensor *k_cache, ta_tensor *v_cache, ta_tensor *k_scale, ta_tensor *v_scale,
+                         const ta_tensor *page_table, const ta_tensor *seq_lens, const ta_tensor *accepted,
+                         const ta_tensor *n_accepted, int32_t tree_size, ta_tensor *seq_lens_out, void *)
+{
+    TAQ8Compact c;
+    const int rc = ta_host_check_q8_compact(k_cache, v_cache, k_scale, v_scale, page_table, seq_lens, accepted, n_accepted,
+                                            tree_size, seq_lens_out, &c);
+    return rc != TA_OK || c.B == 0 ? rc : TA_ERR_HIP;
+}
+
+int tree_attn_q8_fwd(const ta_tensor *q, const ta_tensor *k_cache, const ta_tensor *v_cache, const ta_tensor *k_scale,
+                     const ta_tensor *v_scale, const ta_tensor *page_table, const ta_tensor *seq_lens,
+                     const ta_tensor *tree_parent, ta_tensor *out, ta_tensor *lse, void *, const ta_opts *opts)
+{
+    TAQ8Problem qp;
+    const int rc = ta_host_build_q8_problem(q, k_cache, v_cache, k_scale, v_scale, page_table, seq_lens, tree_parent, out, lse,
+                                            opts, 256, &qp);
+    return rc != TA_OK || qp.pr.p.B == 0 ? rc : TA_ERR_HIP;
+}
+
 int tree_attn_last_status(int32_t *host_status, void *) { return host_status ? TA_ERR_HIP : TA_ERR_NULL; }
 
 int tree_attn_stream_read(const void *buf, size_t bytes, void *sink, void *)

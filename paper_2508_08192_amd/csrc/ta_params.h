@@ -90,6 +90,54 @@ struct TACompact {
     int32_t *status;
 };
 
+// The 8-bit cache: e4m3 codes where TAParams has K and V, and an e8m0 byte per row (strides in elements, i.e. bytes).
+struct TAQ8Params : TAParams {
+    const uint8_t *ks, *vs;            // [num_pages, Hkv, page_size]
+    int64_t ks_sp, ks_sh, ks_ss, vs_sp, vs_sh, vs_ss;
+};
+
+// A step's or a prompt's rows on their way: queries and keys to their positions (rotary embedding), keys and values into the
+// 8-bit cache.  Rows of a token are numbered queries first, then keys, then values.
+struct TARows {
+    const void *q, *k, *v;             // [B, T, H, D]; null: there are none
+    void *q_out, *k_out;               // rotated rows; k_out null: the keys are quantised
+    void *kc, *vc;                     // caches
+    uint8_t *ks, *vs;
+    const float *freqs;                // [R / 2]
+    const int32_t *page_table, *seq_lens, *parent;
+    const unsigned long long *masks_in;
+    int64_t q_sb, q_st, q_sh, k_sb, k_st, k_sh, v_sb, v_st, v_sh;
+    int64_t qo_sb, qo_st, qo_sh, ko_sb, ko_st, ko_sh;
+    int64_t k_sp, k_shc, k_ss, v_sp, v_shc, v_ss, ks_sp, ks_sh, ks_ss, vs_sp, vs_sh, vs_ss;
+    int64_t pt_sb, sl_s, par_sb, masks_sb;
+    int32_t B, T, Hq, Hkv, D, R, ps, capacity, n_pages;
+    int32_t interleaved;
+    float amplitude;
+    int32_t is_bf16;
+    int32_t vec;                       // lanes can take sixteen columns in 16-byte loads
+    int32_t tokens;                    // of one request that a workgroup takes
+    int32_t *status, *status2;
+};
+
+struct TAQ8Read {
+    const void *kc, *vc;
+    const uint8_t *ks, *vs;
+    void *k_out, *v_out;               // [B, N, Hkv, D]
+    const int32_t *page_table, *starts, *counts;
+    int64_t k_sp, k_sh, k_ss, v_sp, v_sh, v_ss, ks_sp, ks_sh, ks_ss, vs_sp, vs_sh, vs_ss;
+    int64_t ko_sb, ko_st, ko_sh, vo_sb, vo_st, vo_sh;
+    int64_t pt_sb, st_s, ct_s;
+    int32_t B, N, Hkv, D, ps, capacity, n_pages;
+    int32_t is_bf16, vec;
+    int32_t tokens;                    // that a workgroup takes
+    int32_t *status;
+};
+
+struct TAQ8Compact : TACompact {
+    uint8_t *ks, *vs;
+    int64_t ks_sp, ks_sh, ks_ss, vs_sp, vs_sh, vs_ss;
+};
+
 // Blocks of the pipelined kernel (gen_sp_block.py).
 #define TA_BLOCKS_PACED 0     // 32x32x16 products, a wait in every steady-state tile
 #define TA_BLOCKS_NARROW 1    // the same without the wait
@@ -137,7 +185,13 @@ struct TAProblem {
                                // part_q15 inside the half of their area that 16-bit rows leave unused
 };
 
-// Host logic shared by every entry point (ta_host.cpp).  None of these touches a device.
+// A call over the 8-bit cache: the same, with the scales beside the parameters.
+struct TAQ8Problem {
+    TAProblem pr;
+    TAQ8Params p;              // filled from pr.p when the workspace is known (ta_host_q8_params)
+};
+
+// Host logic shared by every entry point (ta_host.cpp, ta_q8_host.cpp).  None of these touches a device.
 extern "C++" {
 int ta_host_build_problem(const ta_tensor *q, const ta_tensor *k, const ta_tensor *v, const ta_tensor *pt,
                           const ta_tensor *sl, const ta_tensor *par, const ta_tensor *out, const ta_tensor *lse,
@@ -148,6 +202,27 @@ int ta_host_check_append(const ta_tensor *k_new, const ta_tensor *v_new, const t
 int ta_host_check_compact(const ta_tensor *k_cache, const ta_tensor *v_cache, const ta_tensor *page_table,
                           const ta_tensor *seq_lens, const ta_tensor *accepted, const ta_tensor *n_accepted,
                           int32_t tree_size, const ta_tensor *seq_lens_out, TACompact *c);
+int ta_host_check_rope(const ta_tensor *q, const ta_tensor *k, const ta_tensor *freqs, const ta_tensor *seq_lens,
+                       const ta_tensor *tree_parent, const ta_tensor *q_out, const ta_tensor *k_out, const ta_rope_opts *opts,
+                       TARows *r);
+int ta_host_check_q8_append(const ta_tensor *k_new, const ta_tensor *v_new, const ta_tensor *k_cache, const ta_tensor *v_cache,
+                            const ta_tensor *k_scale, const ta_tensor *v_scale, const ta_tensor *page_table,
+                            const ta_tensor *seq_lens, TARows *r);
+int ta_host_check_q8_rope_append(const ta_tensor *q, const ta_tensor *k_new, const ta_tensor *v_new, const ta_tensor *freqs,
+                                 const ta_tensor *seq_lens, const ta_tensor *tree_parent, const ta_tensor *q_out,
+                                 const ta_tensor *k_cache, const ta_tensor *v_cache, const ta_tensor *k_scale,
+                                 const ta_tensor *v_scale, const ta_tensor *page_table, const ta_rope_opts *opts, TARows *r);
+int ta_host_check_q8_read(const ta_tensor *k_cache, const ta_tensor *v_cache, const ta_tensor *k_scale, const ta_tensor *v_scale,
+                          const ta_tensor *page_table, const ta_tensor *starts, const ta_tensor *counts, const ta_tensor *k_out,
+                          const ta_tensor *v_out, TAQ8Read *r);
+int ta_host_check_q8_compact(const ta_tensor *k_cache, const ta_tensor *v_cache, const ta_tensor *k_scale,
+                             const ta_tensor *v_scale, const ta_tensor *page_table, const ta_tensor *seq_lens,
+                             const ta_tensor *accepted, const ta_tensor *n_accepted, int32_t tree_size,
+                             const ta_tensor *seq_lens_out, TAQ8Compact *c);
+int ta_host_build_q8_problem(const ta_tensor *q, const ta_tensor *k, const ta_tensor *v, const ta_tensor *ks, const ta_tensor *vs,
+                             const ta_tensor *pt, const ta_tensor *sl, const ta_tensor *par, const ta_tensor *out,
+                             const ta_tensor *lse, const ta_opts *opts, int num_cus, TAQ8Problem *pr);
+const TAQ8Params &ta_host_q8_params(TAQ8Problem *pr);
 size_t ta_host_workspace_bytes(int32_t B, int32_t T, int32_t Hq, int32_t Hkv, int32_t D, int32_t dtype, int32_t num_cus);
 void ta_host_fill_plan(const TAProblem &pr, int64_t plan[16]);
 const TADispatchRow *ta_host_dispatch_table(int *n_rows);

@@ -14,9 +14,10 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 # behind it, is loaded that way by the host tests)
 LIB_PATH = os.environ.get("TREEATTN_LIB") or os.path.join(_HERE, "libtreeattn.so")
 
-TA_F32, TA_BF16, TA_I32, TA_U64 = 0, 1, 2, 3
+TA_F32, TA_BF16, TA_I32, TA_U64, TA_E4M3, TA_E8M0 = 0, 1, 2, 3, 4, 5
 TA_KERNEL_AUTO, TA_KERNEL_GENERIC, TA_KERNEL_MFMA, TA_KERNEL_MFMA_BASIC = 0, 1, 2, 3
 TA_STATUS_BAD_PARENT, TA_STATUS_BAD_SEQLEN, TA_STATUS_BAD_PATH, TA_STATUS_BAD_PAGE = 1, 2, 4, 8
+TA_ROPE_PLAIN, TA_ROPE_LINEAR, TA_ROPE_BANDS, TA_ROPE_YARN = 0, 1, 2, 3
 TA_MERGE_GENERAL, TA_MERGE_D128, TA_MERGE_D128_WIDE = 0, 1, 2
 
 TA_OK = 0
@@ -29,6 +30,8 @@ EXPORTS = (
     "tree_attn_encode", "tree_attn_append", "tree_attn_compact", "tree_attn_last_status", "tree_attn_plan",
     "tree_attn_plan_blocks",
     "tree_attn_dispatch_row", "tree_attn_stream_read", "tree_attn_mfma_probe", "tree_attn_fwd_static", "tree_attn_strerror", "tree_attn_version",
+    "tree_attn_rope_freqs", "tree_attn_rope", "tree_attn_q8_append", "tree_attn_q8_rope_append", "tree_attn_q8_read",
+    "tree_attn_q8_compact", "tree_attn_q8_fwd", "tree_attn_q8_plan",
 )
 
 
@@ -58,6 +61,28 @@ class ta_opts(ctypes.Structure):
         ("kv_start", ctypes.c_void_p),
         ("k_new", ctypes.POINTER(ta_tensor)),
         ("v_new", ctypes.POINTER(ta_tensor)),
+        ("status", ctypes.c_void_p),
+    ]
+
+
+class ta_rope_rule(ctypes.Structure):
+    _fields_ = [
+        ("rule", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
+        ("base", ctypes.c_double),
+        ("factor", ctypes.c_double),
+        ("original", ctypes.c_double),
+        ("low", ctypes.c_double),
+        ("high", ctypes.c_double),
+    ]
+
+
+class ta_rope_opts(ctypes.Structure):
+    _fields_ = [
+        ("interleaved", ctypes.c_int32),
+        ("amplitude", ctypes.c_float),
+        ("tree_masks", ctypes.c_void_p),
+        ("tree_masks_stride", ctypes.c_int64),
         ("status", ctypes.c_void_p),
     ]
 
@@ -141,6 +166,19 @@ def load_library():
         lib.tree_attn_strerror.argtypes = [ctypes.c_int]
         lib.tree_attn_version.restype = ctypes.c_int
         lib.tree_attn_version.argtypes = []
+        V = ctypes.c_void_p
+        for name, args in (
+                ("tree_attn_rope_freqs", [ctypes.POINTER(ta_rope_rule), ctypes.c_int32, ctypes.POINTER(ctypes.c_float),
+                                          ctypes.POINTER(ctypes.c_float)]),
+                ("tree_attn_rope", [T] * 7 + [V, ctypes.POINTER(ta_rope_opts)]),
+                ("tree_attn_q8_append", [T] * 8 + [V]),
+                ("tree_attn_q8_rope_append", [T] * 12 + [V, ctypes.POINTER(ta_rope_opts)]),
+                ("tree_attn_q8_read", [T] * 9 + [V]),
+                ("tree_attn_q8_compact", [T] * 8 + [ctypes.c_int32, T, V]),
+                ("tree_attn_q8_fwd", [T] * 10 + [V, ctypes.POINTER(ta_opts)]),
+                ("tree_attn_q8_plan", [T] * 10 + [ctypes.POINTER(ta_opts), ctypes.c_int32, ctypes.POINTER(ctypes.c_int64)])):
+            fn = getattr(lib, name)
+            fn.restype, fn.argtypes = ctypes.c_int, args
         _set_up_call_module(lib)
         _lib = lib
     return _lib
@@ -162,14 +200,17 @@ def _set_up_call_module(lib):
         warnings.warn("_call.so is not built for this Python, calls go through ctypes: run `python -m "
                       "paper_2508_08192_amd.build` (%s)" % e)
         return
-    for name in ("tree_attn_fwd", "tree_attn_fwd_ex", "tree_attn_fwd_static", "tree_attn_append", "tree_attn_compact"):
+    for name in ("tree_attn_fwd", "tree_attn_fwd_ex", "tree_attn_fwd_static", "tree_attn_append", "tree_attn_compact",
+                 "tree_attn_rope", "tree_attn_q8_append", "tree_attn_q8_rope_append", "tree_attn_q8_read",
+                 "tree_attn_q8_compact", "tree_attn_q8_fwd"):
         _entry[name] = ctypes.cast(getattr(lib, name), ctypes.c_void_p).value
     module.setup(torch.Tensor, torch.nn.Parameter, tuple(_dtype_codes(torch).items()))
     _call = module
 
 
 def _dtype_codes(torch):
-    return {torch.float32: TA_F32, torch.bfloat16: TA_BF16, torch.int32: TA_I32, torch.int64: TA_U64, torch.uint64: TA_U64}
+    return {torch.float32: TA_F32, torch.bfloat16: TA_BF16, torch.int32: TA_I32, torch.int64: TA_U64, torch.uint64: TA_U64,
+            torch.float8_e4m3fn: TA_E4M3, torch.float8_e8m0fnu: TA_E8M0}
 
 
 def _torch_dtype_code(t):
@@ -402,6 +443,119 @@ def tree_attn_compact(k_cache, v_cache, page_table, seq_lens, accepted, n_accept
     return rc
 
 
+def tree_attn_rope_freqs(rotary_dim, base=10000.0, rule=TA_ROPE_PLAIN, factor=1.0, original=0.0, low=0.0, high=0.0, check=True):
+    """include/treeattn.h: tree_attn_rope_freqs (host-only).  Returns (list of rotary_dim / 2 frequencies, amplitude), or the
+    negative status if check is False and it failed."""
+    r = ta_rope_rule(int(rule), 0, float(base), float(factor), float(original), float(low), float(high))
+    freqs, amplitude = (ctypes.c_float * max(int(rotary_dim) // 2, 1))(), ctypes.c_float(0.0)
+    rc = load_library().tree_attn_rope_freqs(ctypes.byref(r), int(rotary_dim), freqs, ctypes.byref(amplitude))
+    if rc != TA_OK:
+        if check:
+            raise TreeAttnError(rc, "tree_attn_rope_freqs")
+        return rc
+    return [float(f) for f in freqs], float(amplitude.value)
+
+
+def _rope_opts(interleaved, amplitude, tree_masks, status):
+    o = ta_rope_opts()
+    o.interleaved = int(interleaved)
+    o.amplitude = 0.0 if amplitude is None else float(amplitude)
+    if tree_masks is not None:                         # as in _opts
+        o.tree_masks = tree_masks.data_ptr()
+        o.tree_masks_stride = int(tree_masks.stride(0)) if tree_masks.dim() == 2 else 0
+    if status is not None:
+        o.status = status.ptr if isinstance(status, Desc) else status.data_ptr()
+    return o
+
+
+def _turn(name, tensors, stream, interleaved, amplitude, tree_masks, status, check):
+    lib, rc = load_library(), None
+    if _call is not None and status is None:
+        rc = _call.turn(_entry[name], _stream_address(stream), interleaved, amplitude, tree_masks, *tensors)
+    if rc is None:
+        ds = [_desc(x) for x in tensors]
+        rc = getattr(lib, name)(*[_ref(d) for d in ds], _stream_ptr(stream) if stream != 0 else None,
+                                ctypes.byref(_rope_opts(interleaved, amplitude, tree_masks, status)))
+    if check and rc != TA_OK:
+        raise TreeAttnError(rc, name)
+    return rc
+
+
+def _plain_call(name, tensors, stream, check):
+    lib, rc = load_library(), None
+    if _call is not None:
+        rc = _call.plain(_entry[name], _stream_address(stream), *tensors)
+    if rc is None:
+        ds = [_desc(x) for x in tensors]
+        rc = getattr(lib, name)(*[_ref(d) for d in ds], _stream_ptr(stream) if stream != 0 else None)
+    if check and rc != TA_OK:
+        raise TreeAttnError(rc, name)
+    return rc
+
+
+def tree_attn_rope(q, k, freqs, seq_lens, tree_parent, q_out, k_out, stream=None, interleaved=False, amplitude=None,
+                   tree_masks=None, status=None, check=True):
+    """include/treeattn.h: tree_attn_rope (queries and keys to their positions; tree_parent None: a chunk of a prompt)."""
+    return _turn("tree_attn_rope", (q, k, freqs, seq_lens, tree_parent, q_out, k_out), stream, interleaved, amplitude,
+                 tree_masks, status, check)
+
+
+def tree_attn_q8_append(k_new, v_new, k_cache, v_cache, k_scale, v_scale, page_table, seq_lens, stream=None, check=True):
+    """include/treeattn.h: tree_attn_q8_append (keys and values quantised into the 8-bit cache)."""
+    return _plain_call("tree_attn_q8_append", (k_new, v_new, k_cache, v_cache, k_scale, v_scale, page_table, seq_lens), stream,
+                       check)
+
+
+def tree_attn_q8_rope_append(q, k_new, v_new, freqs, seq_lens, tree_parent, q_out, k_cache, v_cache, k_scale, v_scale,
+                             page_table, stream=None, interleaved=False, amplitude=None, tree_masks=None, status=None,
+                             check=True):
+    """include/treeattn.h: tree_attn_q8_rope_append (tree_attn_rope and tree_attn_q8_append in one launch)."""
+    return _turn("tree_attn_q8_rope_append", (q, k_new, v_new, freqs, seq_lens, tree_parent, q_out, k_cache, v_cache, k_scale,
+                                              v_scale, page_table), stream, interleaved, amplitude, tree_masks, status, check)
+
+
+def tree_attn_q8_read(k_cache, v_cache, k_scale, v_scale, page_table, starts, counts, k_out, v_out, stream=None, check=True):
+    """include/treeattn.h: tree_attn_q8_read (a part of the 8-bit cache as dense rows)."""
+    return _plain_call("tree_attn_q8_read", (k_cache, v_cache, k_scale, v_scale, page_table, starts, counts, k_out, v_out),
+                       stream, check)
+
+
+def tree_attn_q8_compact(k_cache, v_cache, k_scale, v_scale, page_table, seq_lens, accepted, n_accepted, tree_size,
+                         seq_lens_out=None, stream=None, check=True):
+    """include/treeattn.h: tree_attn_q8_compact (tree_attn_compact for the 8-bit cache)."""
+    lib, rc = load_library(), None
+    tensors = (k_cache, v_cache, k_scale, v_scale, page_table, seq_lens, accepted, n_accepted)
+    if _call is not None:
+        rc = _call.q8_compact(_entry["tree_attn_q8_compact"], _stream_address(stream), *tensors, seq_lens_out, tree_size)
+    if rc is None:
+        ds = [_desc(x) for x in tensors]
+        so = _desc(seq_lens_out)
+        rc = lib.tree_attn_q8_compact(*[_ref(d) for d in ds], int(tree_size), _ref(so),
+                                      _stream_ptr(stream) if stream != 0 else None)
+    if check and rc != TA_OK:
+        raise TreeAttnError(rc, "tree_attn_q8_compact")
+    return rc
+
+
+def tree_attn_q8_fwd(q, k_cache, v_cache, k_scale, v_scale, page_table, seq_lens, tree_parent, out, lse=None, stream=None,
+                     scale=None, num_splits=0, kernel=TA_KERNEL_AUTO, workspace=None, events=None, check=True, item_cost=0,
+                     tree_masks=None, kv_start=None, q_node_offset=0, status=None):
+    """include/treeattn.h: tree_attn_q8_fwd (attention over the 8-bit cache)."""
+    lib, rc = load_library(), None
+    tensors = (q, k_cache, v_cache, k_scale, v_scale, page_table, seq_lens, tree_parent, out, lse)
+    if _call is not None and workspace is None and events is None and status is None:
+        rc = _call.q8_fwd(_entry["tree_attn_q8_fwd"], _stream_address(stream), *tensors, scale, num_splits, kernel, item_cost,
+                          tree_masks, kv_start, q_node_offset)
+    if rc is None:
+        ds = [_desc(x) for x in tensors]
+        o = _opts(scale, num_splits, kernel, workspace, events, item_cost, tree_masks, kv_start, q_node_offset, None, None,
+                  status)
+        rc = lib.tree_attn_q8_fwd(*[_ref(d) for d in ds], _stream_ptr(stream) if stream != 0 else None, ctypes.byref(o))
+    if check and rc != TA_OK:
+        raise TreeAttnError(rc, "tree_attn_q8_fwd")
+    return rc
+
+
 def tree_attn_last_status(stream=None):
     """Reads and clears the device status word (synchronises the stream)."""
     val = ctypes.c_int32(0)
@@ -409,6 +563,11 @@ def tree_attn_last_status(stream=None):
     if rc != TA_OK:
         raise TreeAttnError(rc, "tree_attn_last_status")
     return int(val.value)
+
+
+_PLAN_KEYS = ("kernel", "kv_workgroups", "threads", "tile", "row_groups", "rows_per_group", "partial_slots", "merge_workgroups",
+              "min_share", "item_cost", "merge_kernel", "table_row", "workspace_bytes", "partials_q15", "key_split",
+              "workgroup_rows")
 
 
 def tree_attn_plan(q, k_cache, v_cache, page_table, seq_lens, tree_parent, out, lse=None, num_cus=256,
@@ -423,9 +582,20 @@ def tree_attn_plan(q, k_cache, v_cache, page_table, seq_lens, tree_parent, out, 
         if check:
             raise TreeAttnError(rc, "tree_attn_plan")
         return rc
-    keys = ("kernel", "kv_workgroups", "threads", "tile", "row_groups", "rows_per_group", "partial_slots",
-            "merge_workgroups", "min_share", "item_cost", "merge_kernel", "table_row", "workspace_bytes",
-            "partials_q15", "key_split", "workgroup_rows")
-    d = dict(zip(keys, [int(x) for x in plan]))
+    d = dict(zip(_PLAN_KEYS, [int(x) for x in plan]))
     d["blocks"] = int(load_library().tree_attn_plan_blocks(*call))   # the pipelined kernel's: TA_BLOCKS_* of csrc/ta_params.h
     return d
+
+
+def tree_attn_q8_plan(q, k_cache, v_cache, k_scale, v_scale, page_table, seq_lens, tree_parent, out, lse=None, num_cus=256,
+                      scale=None, num_splits=0, kernel=TA_KERNEL_AUTO, check=True, item_cost=0, status=None):
+    """Host-only launch plan of tree_attn_q8_fwd; as tree_attn_plan."""
+    ds = [_desc(x) for x in (q, k_cache, v_cache, k_scale, v_scale, page_table, seq_lens, tree_parent, out, lse)]
+    o = _opts(scale, num_splits, kernel, None, None, item_cost, status=status)
+    plan = (ctypes.c_int64 * 16)()
+    rc = load_library().tree_attn_q8_plan(*[_ref(d) for d in ds], ctypes.byref(o), num_cus, plan)
+    if rc != TA_OK:
+        if check:
+            raise TreeAttnError(rc, "tree_attn_q8_plan")
+        return rc
+    return dict(zip(_PLAN_KEYS, [int(x) for x in plan]))
