@@ -400,7 +400,11 @@ int tree_attn_q8_fwd(const ta_tensor *q, const ta_tensor *k_cache, const ta_tens
     const TAQ8Params &p = ta_host_q8_params(&qp);
     void *const *ev = opts ? opts->events : nullptr;
     auto mark = [&](int i) { return !ev || !ev[i] || hipEventRecord((hipEvent_t)ev[i], st) == hipSuccess; };
-    if (!mark(0) || ta_launch_q8_generic(p, st, dev) != hipSuccess || !mark(1) || ta_launch_merge(p, st) != hipSuccess || !mark(2))
+    if (!mark(0))
+        return TA_ERR_HIP;
+    if ((pr.plan.kernel == TA_KERNEL_MFMA ? ta_launch_q8_mfma(p, st, dev) : ta_launch_q8_generic(p, st, dev)) != hipSuccess || !mark(1))
+        return TA_ERR_HIP;
+    if ((!p.solo && ta_launch_merge(p, st) != hipSuccess) || !mark(2))
         return TA_ERR_HIP;
     return TA_OK;
 }

@@ -65,3 +65,4 @@ hipError_t ta_launch_rows(const TARows &r, hipStream_t stream);
 hipError_t ta_launch_q8_read(const TAQ8Read &r, hipStream_t stream);
 hipError_t ta_launch_q8_compact(const TAQ8Compact &c, hipStream_t stream);
 hipError_t ta_launch_q8_generic(const TAQ8Params &p, hipStream_t stream, int dev);
+hipError_t ta_launch_q8_mfma(const TAQ8Params &p, hipStream_t stream, int dev);

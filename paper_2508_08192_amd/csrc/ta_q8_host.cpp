@@ -207,6 +207,58 @@ int tokens_per_group(int64_t tokens_all, int64_t rows_per_token)
     return n;
 }
 
+// The launch plan of the matrix-core kernel, over that of the scalar one, whose checks have been made.
+int plan_mfma(const ta_tensor *out, const ta_opts *opts, int num_cus, TAProblem *pr)
+{
+    TAParams &p = pr->p;
+    TAPlan &pl = pr->plan;
+    const int num_splits = opts ? opts->num_splits : 0, item_cost = opts ? opts->item_cost : 0;
+    const int64_t lists = (int64_t)p.B * p.Hkv, l1 = lists > 0 ? lists : 1;
+    const int64_t tiles_cap = lists * ((p.capacity - p.T + TA_TILE - 1) / TA_TILE + 1);
+    pl.kernel = TA_KERNEL_MFMA;
+    pl.threads = 512;
+    p.basic = 1;
+    p.ks_rows = pl.ks_rows = p.D == 64 && p.rows > 32 && p.B <= TA_SP_MAX_BATCH ? 64 : 32;   // (the schedule of more does not fit in LDS)
+    const int blocks = (p.rows + p.ks_rows - 1) / p.ks_rows;
+    p.rows_grp = pl.rows_grp = blocks * p.ks_rows;
+    p.n_rg = pl.n_rg = 1;
+    pl.item_cost = item_cost > 0 ? item_cost : lists == 1 ? 6 : 9;
+    p.pad = pl.item_cost - 1;
+    if (tiles_cap + lists * p.pad > INT32_MAX)
+        return TA_ERR_SHAPE;
+    // workgroups side by side, one grid row apart, should fall on one XCD, where the keys come out of the L2 for all but the first
+    int64_t want = num_cus / blocks;
+    if (blocks > 1 && want > 8)
+        want -= want % 8;
+    pl.n_wg = (int)(num_splits > 0 ? num_splits : want > 0 ? want : 1);
+    if (pl.n_wg > tiles_cap)
+        pl.n_wg = (int)(tiles_cap > 0 ? tiles_cap : 1);
+    p.n_wg = pl.n_wg;
+    p.min_q = pl.min_q = 1;
+    pl.n_slots = pl.n_wg + (int)lists;
+    const bool out_aligned = ((uintptr_t)out->data % 16) == 0 && p.o_sb % 4 == 0 && p.o_st % 4 == 0 && p.o_sh % 4 == 0;
+    const int64_t parts = (pl.n_wg + l1 - 1) / l1 + 1;
+    p.merge_kind = !out_aligned ? TA_MERGE_GENERAL : parts >= 13 && lists * p.rows <= 1024 ? TA_MERGE_WIDE : TA_MERGE_ROW;
+    p.part_q15 = 1;
+    p.ls = 2;
+    p.one_parts = 0;
+    if (lists == 1 && num_splits == 0 && p.merge_kind == TA_MERGE_WIDE && pl.n_wg > 8192 / p.D)
+        p.one_parts = 8192 / p.D;
+    pl.merge_kind = p.merge_kind;
+    const int mrows = ta_host_merge_rows(p);
+    pl.merge_wgs = (int)lists * ((p.rows + mrows - 1) / mrows);
+    const size_t rows_total = (size_t)pl.n_slots * p.rows_grp;
+    pr->ws_o_bytes = ta_host_align_up(rows_total * p.D * sizeof(float), 256);
+    pr->ws_lse_bytes = ta_host_align_up(rows_total * sizeof(float), 256);
+    pr->ws_ls_off = ta_host_align_up(rows_total * p.D * 2, 256);
+    pr->ws_bytes = pr->ws_o_bytes + pr->ws_lse_bytes + ta_host_align_up((size_t)lists * 2 * sizeof(int32_t), 256);
+    if (num_splits == 0 && item_cost == 0 && lists > 0 && p.merge_kind != TA_MERGE_GENERAL && tiles_cap / lists <= 18)
+        p.solo = lists * blocks <= num_cus ? TA_SOLO_WIDE : p.ks_rows == 32 ? TA_SOLO_PAIR : 0;
+    if (p.solo)
+        pl.merge_wgs = 0;
+    return TA_OK;
+}
+
 }  // namespace
 
 int ta_host_check_rope(const ta_tensor *q, const ta_tensor *k, const ta_tensor *freqs, const ta_tensor *sl, const ta_tensor *par,
@@ -413,7 +465,12 @@ int ta_host_build_q8_problem(const ta_tensor *q, const ta_tensor *k, const ta_te
     if (opts)
         o = *opts;
     o.kernel = TA_KERNEL_GENERIC;
+    if (o.workspace && (uintptr_t)o.workspace % 256 != 0)
+        return TA_ERR_WORKSPACE;
+    o.workspace = nullptr;                                  // (looked at when the kernel is chosen)
     TAProblem &pr = qp->pr;
+    if (pt && pt->ndim == 2 && pt->shape[1] > INT32_MAX)
+        return TA_ERR_SHAPE;
     int rc = ta_host_build_problem(q, &kq, &vq, pt, sl, par, out, lse, &o, num_cus, &pr);
     if (rc != TA_OK)
         return rc;
@@ -424,9 +481,27 @@ int ta_host_build_q8_problem(const ta_tensor *q, const ta_tensor *k, const ta_te
         return TA_ERR_STRIDE;
     if (pr.p.B > 0 && (!ks->data || !vs->data))
         return TA_ERR_NULL;
-    if (kernel == TA_KERNEL_MFMA || kernel == TA_KERNEL_MFMA_BASIC)
-        return TA_ERR_OPTS;
+    if (pr.p.B > 0 && pr.p.n_pages < 1)
+        return TA_ERR_SHAPE;
     pr.plan.table_row = -1;
+    auto in_32_bits = [](const ta_tensor *t) { return t->stride[0] < INT32_MAX && t->stride[2] < INT32_MAX; };
+    const bool mfma_ok = q->dtype == TA_BF16 && (pr.p.D == 64 || pr.p.D == 128) && (!pt || pr.p.ps_shift >= 4) && pr.p.G <= 256 &&
+                         on_16_bytes(q) && on_16_bytes(k) && on_16_bytes(v) && in_32_bits(k) && in_32_bits(v) && in_32_bits(ks) &&
+                         in_32_bits(vs);
+    if (!mfma_ok && (kernel == TA_KERNEL_MFMA || kernel == TA_KERNEL_MFMA_BASIC))
+        return TA_ERR_OPTS;
+    if (mfma_ok && kernel != TA_KERNEL_GENERIC) {
+        rc = plan_mfma(out, opts, num_cus, &pr);
+        if (rc != TA_OK)
+            return rc;
+    }
+    if (opts && opts->workspace) {
+        if (opts->workspace_bytes < pr.ws_bytes)
+            return TA_ERR_WORKSPACE;
+        pr.p.ws_o = (float *)opts->workspace;
+        pr.p.ws_lse = (float *)((char *)opts->workspace + pr.ws_ls_off);
+        pr.p.ws_parts = (int32_t *)((char *)opts->workspace + pr.ws_o_bytes + pr.ws_lse_bytes);
+    }
     TAQ8Params &p = qp->p;
     memset(&p, 0, sizeof p);
     p.ks = (const uint8_t *)ks->data; p.vs = (const uint8_t *)vs->data;
