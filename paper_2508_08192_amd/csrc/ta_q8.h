@@ -5,6 +5,8 @@
 
 typedef float q8_f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 q8_bf16x2 __attribute__((ext_vector_type(2)));
+typedef short q8_s16x2 __attribute__((ext_vector_type(2)));
+typedef unsigned short q8_u16x2 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ float q8_scale(uint32_t byte)               // 2^(byte - 127); 255: NaN
 {
@@ -20,9 +22,9 @@ __device__ __forceinline__ uint32_t q8_scale_byte(uint32_t top)
     return top == 0u ? 127u : (uint32_t)(e < 1 ? 1 : e);
 }
 
-__device__ __forceinline__ float q8_inverse(uint32_t byte)             // 2^(127 - byte) for the bytes that are written, 1 .. 247
+__device__ __forceinline__ float q8_power(uint32_t byte)               // 2^(byte - 127) for the bytes that are written, 1 .. 247
 {
-    return __uint_as_float((254u - byte) << 23);
+    return __uint_as_float(byte << 23);
 }
 
 __device__ __forceinline__ uint32_t q8_finite_bits(float x)            // |x| as bits, 0 for an infinity or a NaN
@@ -31,17 +33,29 @@ __device__ __forceinline__ uint32_t q8_finite_bits(float x)            // |x| as
     return u < 0x7f800000u ? u : 0u;
 }
 
-__device__ __forceinline__ float q8_no_inf(float x)
+// Values over a power of two as codes, to nearest, ties to even; what is no number (or above 464 of it) becomes a NaN.  The
+// instructions were compared with the definition on all bf16 values and as many fp32 ones at seven powers from 2^-126 to 2^120.
+__device__ __forceinline__ uint32_t q8_codes4(float a, float b, float c, float d, float power)
 {
-    return (__float_as_uint(x) & 0x7fffffffu) == 0x7f800000u ? __uint_as_float(0x7fc00000u) : x;
+    q8_s16x2 r = {0, 0};
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, a, b, power, false);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, c, d, power, true);
+    return __builtin_bit_cast(uint32_t, r);
 }
 
-// Four values of at most 448 as codes, to nearest, ties to even.
-__device__ __forceinline__ uint32_t q8_codes4(float a, float b, float c, float d)
+__device__ __forceinline__ uint32_t q8_codes4(uint32_t lo, uint32_t hi, float power)       // of two pairs of bf16 values
 {
-    int r = __builtin_amdgcn_cvt_pk_fp8_f32(q8_no_inf(a), q8_no_inf(b), 0, false);
-    r = __builtin_amdgcn_cvt_pk_fp8_f32(q8_no_inf(c), q8_no_inf(d), r, true);
-    return (uint32_t)r;
+    q8_s16x2 r = {0, 0};
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(q8_bf16x2, lo), power, false);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(q8_bf16x2, hi), power, true);
+    return __builtin_bit_cast(uint32_t, r);
+}
+
+// Two codes times a power of two as bf16 (lower or upper half of the word).
+template <bool UPPER>
+__device__ __forceinline__ uint32_t q8_bf16_2(uint32_t codes, float power)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)codes, power, UPPER));
 }
 
 __device__ __forceinline__ void q8_values4(uint32_t codes, float v[4])

@@ -70,112 +70,134 @@ __device__ __forceinline__ RowsPlace rows_place(const TARows &a, int b, int pos)
     return r;
 }
 
-// The row x of token t: where it comes from and what it is.
-struct RowsRow {
-    const void *src;
-    int h;
+// A row of every token (query, key or value head): where it comes from and goes to, but for the token.  The strides' unit is a byte.
+struct RowsHead {
     int kind;                               // 0 query, 1 key, 2 value
+    const char *src;
+    int64_t src_st;
+    char *dense;                            // rotated rows; null: into the cache
+    int64_t dense_st;
+    char *codes;
+    int64_t code_sp, code_ss;
+    uint8_t *scale;
+    int64_t scale_sp, scale_ss;
 };
 
-template <bool BF16>
-__device__ __forceinline__ RowsRow rows_row(const TARows &a, int b, int t, int x)
+template <bool BF16, bool QUANT>
+__device__ __forceinline__ RowsHead rows_head(const TARows &a, int b, int y)
 {
     constexpr int ES = BF16 ? 2 : 4;
-    RowsRow r;
-    r.kind = x < a.Hq ? 0 : x < a.Hq + a.Hkv ? 1 : 2;
-    r.h = r.kind == 0 ? x : r.kind == 1 ? x - a.Hq : x - a.Hq - a.Hkv;
-    const char *base = (const char *)(r.kind == 0 ? a.q : r.kind == 1 ? a.k : a.v);
-    const int64_t sb = r.kind == 0 ? a.q_sb : r.kind == 1 ? a.k_sb : a.v_sb, st = r.kind == 0 ? a.q_st : r.kind == 1 ? a.k_st : a.v_st,
-                  sh = r.kind == 0 ? a.q_sh : r.kind == 1 ? a.k_sh : a.v_sh;
-    r.src = base + ((int64_t)b * sb + (int64_t)t * st + (int64_t)r.h * sh) * ES;
+    RowsHead r = {};
+    r.kind = y < a.Hq ? 0 : y < a.Hq + a.Hkv ? 1 : 2;
+    const int64_t h = r.kind == 0 ? y : r.kind == 1 ? y - a.Hq : y - a.Hq - a.Hkv;
+    if (r.kind == 0) {
+        r.src = (const char *)a.q + (b * a.q_sb + h * a.q_sh) * ES;
+        r.src_st = a.q_st * ES;
+        r.dense = (char *)a.q_out + (b * a.qo_sb + h * a.qo_sh) * ES;
+        r.dense_st = a.qo_st * ES;
+    } else if (r.kind == 1) {
+        r.src = (const char *)a.k + (b * a.k_sb + h * a.k_sh) * ES;
+        r.src_st = a.k_st * ES;
+        if (QUANT) {
+            r.codes = (char *)a.kc + h * a.k_shc;
+            r.code_sp = a.k_sp;
+            r.code_ss = a.k_ss;
+            r.scale = a.ks + h * a.ks_sh;
+            r.scale_sp = a.ks_sp;
+            r.scale_ss = a.ks_ss;
+        } else {
+            r.dense = (char *)a.k_out + (b * a.ko_sb + h * a.ko_sh) * ES;
+            r.dense_st = a.ko_st * ES;
+        }
+    } else {
+        r.src = (const char *)a.v + (b * a.v_sb + h * a.v_sh) * ES;
+        r.src_st = a.v_st * ES;
+        r.codes = (char *)a.vc + h * a.v_shc;
+        r.code_sp = a.v_sp;
+        r.code_ss = a.v_ss;
+        r.scale = a.vs + h * a.vs_sh;
+        r.scale_sp = a.vs_sp;
+        r.scale_ss = a.vs_ss;
+    }
     return r;
 }
 
-template <bool BF16>
-__device__ __forceinline__ char *rows_dense(const TARows &a, int b, int t, const RowsRow &r)
-{
-    constexpr int ES = BF16 ? 2 : 4;
-    return r.kind == 0 ? (char *)a.q_out + ((int64_t)b * a.qo_sb + (int64_t)t * a.qo_st + (int64_t)r.h * a.qo_sh) * ES
-                       : (char *)a.k_out + ((int64_t)b * a.ko_sb + (int64_t)t * a.ko_st + (int64_t)r.h * a.ko_sh) * ES;
-}
-
-__device__ __forceinline__ char *rows_codes(const TARows &a, const RowsPlace &at, const RowsRow &r)
-{
-    return r.kind == 1 ? (char *)a.kc + at.page * a.k_sp + (int64_t)r.h * a.k_shc + at.slot * a.k_ss
-                       : (char *)a.vc + at.page * a.v_sp + (int64_t)r.h * a.v_shc + at.slot * a.v_ss;
-}
-
-__device__ __forceinline__ uint8_t *rows_scale(const TARows &a, const RowsPlace &at, const RowsRow &r)
-{
-    return r.kind == 1 ? a.ks + at.page * a.ks_sp + (int64_t)r.h * a.ks_sh + at.slot * a.ks_ss
-                       : a.vs + at.page * a.vs_sp + (int64_t)r.h * a.vs_sh + at.slot * a.vs_ss;
-}
+// How a lane's columns pair up.
+enum { ROWS_KEEP, ROWS_HALVES, ROWS_NEIGHBOURS };      // not at all; column j with j + R/2; 2j with 2j + 1
 
 // Rotated (TURN) queries and keys to dense rows, or keys (rotated or not) and values into the cache (QUANT).  A lane holds sixteen
-// columns of a row in two runs of eight, which are each other's partners where columns are paired across the halves, and
-// neighbours otherwise; the LPR lanes of a row find its maximum among themselves.
-template <bool BF16, bool TURN, bool QUANT, int LPR>
+// columns of a row in two runs of eight, half of the rotated (or of the other) columns apart: each load and store of the lanes of a
+// row is then one piece of memory, and columns that pair up across the halves meet in one lane.  The LPR lanes of a row find its
+// maximum among themselves.  A thread keeps its head and goes from token to token, ROWS_AHEAD of them requested at a time.
+// What bounds it: bytes in flight, and the round trips of a workgroup's start (length and tree, then the page).
+constexpr int ROWS_AHEAD = 4;
+
+template <bool BF16, int TURN, bool QUANT, int LPR>
 __global__ __launch_bounds__(ROWS_THREADS) void ta_rows_kernel(TARows a)
 {
-    constexpr int V = BF16 ? 1 : 2;                        // 16-byte loads of eight columns
+    constexpr int V = BF16 ? 1 : 2, ES = BF16 ? 2 : 4;     // 16-byte loads of eight columns, bytes of an element
+    constexpr int RPP = ROWS_THREADS / LPR;                // rows at a time
     __shared__ float2 turn[TURN ? ROWS_TOKENS : 1][TURN ? TA_MAX_HEAD_DIM / 2 : 1];
     __shared__ RowsPlace place[ROWS_TOKENS];
     __shared__ int depths[TURN ? TA_WAVE : 1];
-    const int b = blockIdx.y, tid = threadIdx.x, c = tid % LPR;
+    const int b = blockIdx.y, tid = threadIdx.x, c = tid % LPR, slot = tid / LPR;
     const int L = a.seq_lens[(int64_t)b * a.sl_s];
     const int half = a.R / 2;
     const int rows_tok = a.Hq + (QUANT ? 2 : 1) * a.Hkv;
-    bool bad_tree = false;
-    if (TURN && a.parent) {
-        const int depth = rows_depth(a, b, tid & 63, bad_tree);
-        if (tid < TA_WAVE)
-            depths[tid] = depth;
-    }
-    const bool bad_len = L < 0 || (QUANT && (int64_t)L + a.T > (int64_t)a.capacity);
-    const bool bad = bad_len || bad_tree;
-    if (bad && tid == 0 && blockIdx.x == 0) {
-        const int bits = (bad_len ? TA_STATUS_BAD_SEQLEN : 0) | (bad_tree ? TA_STATUS_BAD_PARENT : 0);
-        atomicOr(a.status, bits);
-        if (a.status2)
-            atomicOr(a.status2, bits);
-    }
-    if (bad && !TURN)
-        return;
+    const bool live = 16 * c < a.D;
+    // columns of the lane's two runs in a rotated row, and in one that is taken as it is
+    const bool turned = TURN && c < a.R / 16;
+    const int t_c0 = turned ? 8 * c : a.R + 8 * (c - a.R / 16), t_c1 = t_c0 + (turned ? half : (a.D - a.R) / 2);
+    const int v_c0 = 8 * c, v_c1 = 8 * c + a.D / 2;
     const int groups = (a.T + a.tokens - 1) / a.tokens;
+    const float freq0 = TURN ? a.freqs[tid % half] : 0.f;  // of this thread's first entry of the table
+    bool bad = false;
     for (int grp = blockIdx.x; grp < groups; grp += gridDim.x) {
-        const int t0 = grp * a.tokens, n = min(a.tokens, a.T - t0), total = n * rows_tok;
-        uint4 raw[2][V];
-        RowsRow row;
-        int tok = 0;
-        // columns of the lane's two runs
-        const bool turned_cols = TURN && c < a.R / 16;
-        auto columns = [&](bool value, int &c0, int &c1) {
-            const bool apart = turned_cols && !a.interleaved && !value;
-            c0 = apart ? 8 * c : 16 * c;
-            c1 = apart ? half + 8 * c : 16 * c + 8;
-        };
-        auto fetch = [&](int x) {
-            tok = x / rows_tok;
-            row = rows_row<BF16>(a, b, t0 + tok, x - tok * rows_tok);
-            int c0, c1;
-            columns(row.kind == 2, c0, c1);
-            if (16 * c < a.D) {
+        const int t0 = grp * a.tokens, n = min(a.tokens, a.T - t0);
+        uint4 raw[ROWS_AHEAD][2][V];
+        // a block of heads: as many as the workgroup has rows at a time, and the last one of fewer takes several tokens at a time
+        int m = min(RPP, rows_tok), tpp = RPP / m, tok0 = slot / m;
+        RowsHead row = rows_head<BF16, QUANT>(a, b, slot - tok0 * m);
+        bool as_is = !TURN || row.kind == 2;
+        int c0 = as_is ? v_c0 : t_c0, c1 = as_is ? v_c1 : t_c1;
+        auto fetch = [&](int tok) {
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    raw[0][v] = *(const uint4 *)((const char *)row.src + c0 * (BF16 ? 2 : 4) + 16 * v);
-                    raw[1][v] = *(const uint4 *)((const char *)row.src + c1 * (BF16 ? 2 : 4) + 16 * v);
+            for (int u = 0; u < ROWS_AHEAD; ++u)
+                if (live && tok + u * tpp < n) {
+                    const char *src = row.src + (t0 + tok + u * tpp) * row.src_st;
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        raw[u][0][v] = *(const uint4 *)(src + c0 * ES + 16 * v);
+                        raw[u][1][v] = *(const uint4 *)(src + c1 * ES + 16 * v);
+                    }
                 }
-            }
         };
-        int x = tid / LPR;
-        if (x < total)
-            fetch(x);
+        if (tok0 < tpp)
+            fetch(tok0);                                   // (on its way while the length and the tree arrive)
+        if (grp == (int)blockIdx.x) {
+            bool bad_tree = false;
+            if (TURN && a.parent) {
+                const int depth = rows_depth(a, b, tid & 63, bad_tree);
+                if (tid < TA_WAVE)
+                    depths[tid] = depth;
+            }
+            const bool bad_len = L < 0 || (QUANT && (int64_t)L + a.T > (int64_t)a.capacity);
+            bad = bad_len || bad_tree;
+            if (bad && tid == 0 && blockIdx.x == 0) {
+                const int bits = (bad_len ? TA_STATUS_BAD_SEQLEN : 0) | (bad_tree ? TA_STATUS_BAD_PARENT : 0);
+                atomicOr(a.status, bits);
+                if (a.status2)
+                    atomicOr(a.status2, bits);
+            }
+            if (bad && !TURN)
+                return;
+        }
         __syncthreads();                                   // the tables of the group before are no longer read
         if (TURN && !bad)
             for (int k = tid; k < n * half; k += ROWS_THREADS) {
                 const int i = k / half, j = k - i * half;
                 const int d = a.parent ? depths[t0 + i] : t0 + i;
-                turn[i][j] = rows_turn((double)L + (double)d, a.freqs[j], a.amplitude);
+                turn[i][j] = rows_turn((double)L + (double)d, k == tid ? freq0 : a.freqs[j], a.amplitude);
             }
         if (QUANT && !bad && tid < n) {
             place[tid] = rows_place(a, b, L + t0 + tid);
@@ -186,91 +208,130 @@ __global__ __launch_bounds__(ROWS_THREADS) void ta_rows_kernel(TARows a)
             }
         }
         __syncthreads();
-        for (; x < total; x += ROWS_THREADS / LPR) {
-            if (x >= ROWS_THREADS / LPR)
-                fetch(x);
-            const bool live = 16 * c < a.D;
-            float e[2][8];
+        for (int y0 = 0; y0 < rows_tok; y0 += RPP) {
+            if (y0 > 0) {
+                m = min(RPP, rows_tok - y0);
+                tpp = RPP / m;
+                tok0 = slot / m;
+                row = rows_head<BF16, QUANT>(a, b, y0 + slot - tok0 * m);
+                as_is = !TURN || row.kind == 2;
+                c0 = as_is ? v_c0 : t_c0;
+                c1 = as_is ? v_c1 : t_c1;
+            }
+            for (int tok1 = tok0; tok1 < n && tok0 < tpp; tok1 += ROWS_AHEAD * tpp) {
+                if (y0 > 0 || tok1 > tok0)
+                    fetch(tok1);
 #pragma unroll
-            for (int r = 0; r < 2; ++r)
+                for (int u = 0; u < ROWS_AHEAD; ++u) {
+                    const int tok = tok1 + u * tpp;
+                    if (tok >= n)
+                        break;
+                    // the row's columns: fp32 values where they are turned or are fp32, pairs of bf16 where those are enough
+                    float e[2][8];
+                    uint32_t pair[2][4];
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const uint32_t w[4] = {raw[r][v].x, raw[r][v].y, raw[r][v].z, raw[r][v].w};
+                    for (int r = 0; r < 2; ++r)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        if (BF16) {
-                            e[r][2 * i] = live ? __uint_as_float(w[i] << 16) : 0.f;
-                            e[r][2 * i + 1] = live ? __uint_as_float(w[i] & 0xffff0000u) : 0.f;
+                        for (int v = 0; v < V; ++v) {
+                            const uint32_t w[4] = {raw[u][r][v].x, raw[u][r][v].y, raw[u][r][v].z, raw[u][r][v].w};
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                if (BF16) {
+                                    pair[r][i] = live ? w[i] : 0u;
+                                    e[r][2 * i] = __uint_as_float(pair[r][i] << 16);
+                                    e[r][2 * i + 1] = __uint_as_float(pair[r][i] & 0xffff0000u);
+                                } else {
+                                    e[r][4 * v + i] = live ? __uint_as_float(w[i]) : 0.f;
+                                }
+                            }
+                        }
+                    if (TURN && turned && !as_is && !bad) {
+                        if (TURN == ROWS_HALVES) {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i)
+                                rows_rotate(e[0][i], e[1][i], turn[tok][c0 + i]);
                         } else {
-                            e[r][4 * v + i] = live ? __uint_as_float(w[i]) : 0.f;
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                rows_rotate(e[0][2 * i], e[0][2 * i + 1], turn[tok][c0 / 2 + i]);
+                                rows_rotate(e[1][2 * i], e[1][2 * i + 1], turn[tok][c1 / 2 + i]);
+                            }
+                        }
+                        if (BF16) {
+#pragma unroll
+                            for (int r = 0; r < 2; ++r)
+#pragma unroll
+                                for (int i = 0; i < 4; ++i)
+                                    pair[r][i] = q8_pack_bf16(e[r][2 * i], e[r][2 * i + 1]);
                         }
                     }
-                }
-            int c0, c1;
-            columns(row.kind == 2, c0, c1);
-            if (TURN && turned_cols && row.kind != 2) {
+                    if (TURN && (row.kind == 0 || !QUANT) && live) {
+                        char *dst = row.dense + (t0 + tok) * row.dense_st;
+                        if (BF16) {
+                            const uint4 nan = make_uint4(0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u);
+                            *(uint4 *)(dst + 2 * c0) = bad ? nan : make_uint4(pair[0][0], pair[0][1], pair[0][2], pair[0][3]);
+                            *(uint4 *)(dst + 2 * c1) = bad ? nan : make_uint4(pair[1][0], pair[1][1], pair[1][2], pair[1][3]);
+                        } else {
+                            const float nan = __uint_as_float(0x7fc00000u);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float2 t = bad ? make_float2(__uint_as_float(0x7fc00000u), 0.f) : turn[tok][8 * c + i];
-                    // (the pair of frequency 8 c + i: columns i of both runs, or neighbours within one of them)
-                    float &p0 = a.interleaved ? e[i / 4][(2 * i) % 8] : e[0][i], &p1 = a.interleaved ? e[i / 4][(2 * i) % 8 + 1] : e[1][i];
-                    rows_rotate(p0, p1, t);
-                }
-            }
-            uint32_t packed[2][4];                         // bf16 rows: what is stored, and what is quantised
-            if (TURN && BF16) {
-#pragma unroll
-                for (int r = 0; r < 2; ++r)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        packed[r][i] = q8_pack_bf16(e[r][2 * i], e[r][2 * i + 1]);
-                        if (bad)
-                            packed[r][i] = 0x7fc07fc0u;
-                        if (QUANT) {
-                            e[r][2 * i] = __uint_as_float(packed[r][i] << 16);
-                            e[r][2 * i + 1] = __uint_as_float(packed[r][i] & 0xffff0000u);
+                            for (int v = 0; v < 2; ++v) {
+                                *(float4 *)(dst + 4 * c0 + 16 * v) = bad ? make_float4(nan, nan, nan, nan)
+                                    : make_float4(e[0][4 * v], e[0][4 * v + 1], e[0][4 * v + 2], e[0][4 * v + 3]);
+                                *(float4 *)(dst + 4 * c1 + 16 * v) = bad ? make_float4(nan, nan, nan, nan)
+                                    : make_float4(e[1][4 * v], e[1][4 * v + 1], e[1][4 * v + 2], e[1][4 * v + 3]);
+                            }
                         }
                     }
-            }
-            if (TURN && (row.kind == 0 || !QUANT)) {
-                char *dst = rows_dense<BF16>(a, b, t0 + tok, row);
-                if (live) {
-                    if (BF16) {
-                        *(uint4 *)(dst + 2 * c0) = make_uint4(packed[0][0], packed[0][1], packed[0][2], packed[0][3]);
-                        *(uint4 *)(dst + 2 * c1) = make_uint4(packed[1][0], packed[1][1], packed[1][2], packed[1][3]);
-                    } else {
-                        const float nan = __uint_as_float(0x7fc00000u);
+                    if (QUANT && row.kind != 0) {              // (all lanes of a row are in here or none)
+                        // the largest magnitude, as bits, which order as the values do; two bf16 at a time
+                        auto over_row = [&](uint32_t top) {
 #pragma unroll
-                        for (int v = 0; v < 2; ++v) {
-                            *(float4 *)(dst + 4 * c0 + 16 * v) = bad ? make_float4(nan, nan, nan, nan)
-                                : make_float4(e[0][4 * v], e[0][4 * v + 1], e[0][4 * v + 2], e[0][4 * v + 3]);
-                            *(float4 *)(dst + 4 * c1 + 16 * v) = bad ? make_float4(nan, nan, nan, nan)
-                                : make_float4(e[1][4 * v], e[1][4 * v + 1], e[1][4 * v + 2], e[1][4 * v + 3]);
+                            for (int off = LPR / 2; off > 0; off >>= 1)
+                                top = max(top, (uint32_t)__shfl_xor((int)top, off, TA_WAVE));
+                            return top;
+                        };
+                        uint32_t top = 0;
+                        if (BF16) {
+                            q8_u16x2 m = {0, 0};
+#pragma unroll
+                            for (int i = 0; i < 8; ++i)
+                                m = __builtin_elementwise_max(m, __builtin_bit_cast(q8_u16x2, pair[i / 4][i % 4] & 0x7fff7fffu));
+                            top = (uint32_t)max(m.x, m.y) << 16;
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 16; ++i)
+                                top = max(top, __float_as_uint(e[i / 8][i % 8]) & 0x7fffffffu);
+                        }
+                        top = over_row(top);
+                        if (top >= 0x7f800000u) {              // no number among them: the largest of the others
+                            top = 0;
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                if (BF16)
+                                    top = max(top, max(q8_finite_bits(__uint_as_float(pair[i / 4][i % 4] << 16)),
+                                                       q8_finite_bits(__uint_as_float(pair[i / 4][i % 4] & 0xffff0000u))));
+                                else
+                                    top = max(top, max(q8_finite_bits(e[i / 4][2 * (i % 4)]), q8_finite_bits(e[i / 4][2 * (i % 4) + 1])));
+                            }
+                            top = over_row(top);
+                        }
+                        if (!bad && place[tok].page >= 0) {
+                            const RowsPlace at = place[tok];
+                            const uint32_t byte = q8_scale_byte(top);
+                            const float power = q8_power(byte);
+                            char *dst = row.codes + at.page * row.code_sp + at.slot * row.code_ss;
+                            if (live) {
+#pragma unroll
+                                for (int r = 0; r < 2; ++r)
+                                    *(uint2 *)(dst + (r ? c1 : c0)) =
+                                        BF16 ? make_uint2(q8_codes4(pair[r][0], pair[r][1], power), q8_codes4(pair[r][2], pair[r][3], power))
+                                             : make_uint2(q8_codes4(e[r][0], e[r][1], e[r][2], e[r][3], power),
+                                                          q8_codes4(e[r][4], e[r][5], e[r][6], e[r][7], power));
+                            }
+                            if (c == 0)
+                                row.scale[at.page * row.scale_sp + at.slot * row.scale_ss] = (uint8_t)byte;
                         }
                     }
-                }
-            }
-            if (QUANT) {
-                uint32_t top = 0;
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    top = max(top, q8_finite_bits(e[i / 8][i % 8]));
-                for (int off = LPR / 2; off > 0; off >>= 1)
-                    top = max(top, (uint32_t)__shfl_xor((int)top, off, TA_WAVE));
-                if (row.kind != 0 && !bad && place[tok].page >= 0) {
-                    const RowsPlace at = place[tok];
-                    const uint32_t byte = q8_scale_byte(top);
-                    const float inv = q8_inverse(byte);
-                    char *dst = rows_codes(a, at, row);
-                    if (live) {
-#pragma unroll
-                        for (int r = 0; r < 2; ++r)
-                            *(uint2 *)(dst + (r ? c1 : c0)) =
-                                make_uint2(q8_codes4(e[r][0] * inv, e[r][1] * inv, e[r][2] * inv, e[r][3] * inv),
-                                           q8_codes4(e[r][4] * inv, e[r][5] * inv, e[r][6] * inv, e[r][7] * inv));
-                    }
-                    if (c == 0)
-                        *rows_scale(a, at, row) = (uint8_t)byte;
                 }
             }
         }
@@ -320,7 +381,8 @@ __global__ __launch_bounds__(ROWS_THREADS) void ta_rows_any_kernel(TARows a)
             if (TURN && lane + k * TA_WAVE < half)
                 cs[k] = rows_turn((double)L + (double)d, a.freqs[lane + k * TA_WAVE], a.amplitude);
         for (int x = wave; x < rows_tok; x += ROWS_THREADS / TA_WAVE) {
-            const RowsRow row = rows_row<BF16>(a, b, t, x);
+            const RowsHead row = rows_head<BF16, QUANT>(a, b, x);
+            const char *src = row.src + t * row.src_st;
             // values: no pairs, all columns are others
             const bool pairs = TURN && row.kind != 2;
             const int h = pairs ? half : 0, r0 = 2 * h, nr = pairs ? rest : a.D;
@@ -338,7 +400,7 @@ __global__ __launch_bounds__(ROWS_THREADS) void ta_rows_any_kernel(TARows a)
                 col[2 * P + k] = lane + k * TA_WAVE < nr ? r0 + lane + k * TA_WAVE : -1;
 #pragma unroll
             for (int k = 0; k < 2 * P + N; ++k)
-                e[k] = col[k] >= 0 ? load(row.src, col[k]) : 0.f;
+                e[k] = col[k] >= 0 ? load(src, col[k]) : 0.f;
             if (pairs) {
 #pragma unroll
                 for (int k = 0; k < P; ++k)
@@ -346,7 +408,7 @@ __global__ __launch_bounds__(ROWS_THREADS) void ta_rows_any_kernel(TARows a)
                         rows_rotate(e[2 * k], e[2 * k + 1], cs[k]);
             }
             if (TURN && (row.kind == 0 || !QUANT)) {
-                char *dst = rows_dense<BF16>(a, b, t, row);
+                char *dst = row.dense + t * row.dense_st;
 #pragma unroll
                 for (int k = 0; k < 2 * P + N; ++k)
                     if (col[k] >= 0) {
@@ -367,20 +429,19 @@ __global__ __launch_bounds__(ROWS_THREADS) void ta_rows_any_kernel(TARows a)
                 for (int off = TA_WAVE / 2; off > 0; off >>= 1)
                     top = max(top, (uint32_t)__shfl_xor((int)top, off, TA_WAVE));
                 const uint32_t byte = q8_scale_byte(top);
-                const float inv = q8_inverse(byte);
-                char *dst = rows_codes(a, at, row);
+                char *dst = row.codes + at.page * row.code_sp + at.slot * row.code_ss;
 #pragma unroll
                 for (int k = 0; k < 2 * P + N; ++k)
                     if (col[k] >= 0)
-                        ((uint8_t *)dst)[col[k]] = (uint8_t)q8_codes4(e[k] * inv, 0.f, 0.f, 0.f);
+                        ((uint8_t *)dst)[col[k]] = (uint8_t)q8_codes4(e[k], 0.f, 0.f, 0.f, q8_power(byte));
                 if (lane == 0)
-                    *rows_scale(a, at, row) = (uint8_t)byte;
+                    row.scale[at.page * row.scale_sp + at.slot * row.scale_ss] = (uint8_t)byte;
             }
         }
     }
 }
 
-template <bool BF16, bool TURN, bool QUANT>
+template <bool BF16, int TURN, bool QUANT>
 static hipError_t launch_rows(const TARows &r, hipStream_t stream)
 {
     const int tokens = r.vec ? r.tokens : 1, groups = (r.T + tokens - 1) / tokens;
@@ -388,7 +449,7 @@ static hipError_t launch_rows(const TARows &r, hipStream_t stream)
         return hipErrorInvalidValue;
     const dim3 grid(groups < 65536 ? groups : 65536, r.B), block(ROWS_THREADS);
     if (!r.vec)
-        hipLaunchKernelGGL((ta_rows_any_kernel<BF16, TURN, QUANT>), grid, block, 0, stream, r);
+        hipLaunchKernelGGL((ta_rows_any_kernel<BF16, TURN != ROWS_KEEP, QUANT>), grid, block, 0, stream, r);
     else if (r.D <= 16 * 4)
         hipLaunchKernelGGL((ta_rows_kernel<BF16, TURN, QUANT, 4>), grid, block, 0, stream, r);
     else if (r.D <= 16 * 8)
@@ -398,98 +459,136 @@ static hipError_t launch_rows(const TARows &r, hipStream_t stream)
     return hipGetLastError();
 }
 
-hipError_t ta_launch_rows(const TARows &r, hipStream_t stream)
+template <bool BF16>
+static hipError_t launch_rows(const TARows &r, hipStream_t stream)
 {
     const bool turn = r.freqs != nullptr, quant = r.k_out == nullptr && r.kc != nullptr;
     if (turn && quant)
-        return r.is_bf16 ? launch_rows<true, true, true>(r, stream) : launch_rows<false, true, true>(r, stream);
+        return r.interleaved ? launch_rows<BF16, ROWS_NEIGHBOURS, true>(r, stream) : launch_rows<BF16, ROWS_HALVES, true>(r, stream);
     if (turn)
-        return r.is_bf16 ? launch_rows<true, true, false>(r, stream) : launch_rows<false, true, false>(r, stream);
-    return r.is_bf16 ? launch_rows<true, false, true>(r, stream) : launch_rows<false, false, true>(r, stream);
+        return r.interleaved ? launch_rows<BF16, ROWS_NEIGHBOURS, false>(r, stream) : launch_rows<BF16, ROWS_HALVES, false>(r, stream);
+    return launch_rows<BF16, ROWS_KEEP, true>(r, stream);
 }
 
-// Rows of the cache as dense ones.  A lane takes sixteen codes (or, VEC false, one).
-template <bool BF16, bool VEC>
+hipError_t ta_launch_rows(const TARows &r, hipStream_t stream)
+{
+    return r.is_bf16 ? launch_rows<true>(r, stream) : launch_rows<false>(r, stream);
+}
+
+// Rows of the cache as dense ones.  The LPR lanes of a row take as many codes each as fill 16 bytes of output (PER; or one code,
+// where rows do not start on 16 bytes), so that a row is written as one piece of memory.  What bounds it: the writes; a thread
+// requests READ_AHEAD pieces before it writes the first (one after the other, 16 contexts of 1000 to 9000 tokens took 117 us).
+constexpr int READ_AHEAD = 8, READ_TOKENS = 32;
+
+template <bool BF16, int PER, int LPR>
 __global__ __launch_bounds__(ROWS_THREADS) void ta_q8_read_kernel(TAQ8Read a)
 {
-    constexpr int ES = BF16 ? 2 : 4, PER = VEC ? 16 : 1;
-    const int b = blockIdx.y;
+    constexpr int ES = BF16 ? 2 : 4, RPP = ROWS_THREADS / LPR;
+    __shared__ RowsPlace place[READ_TOKENS];
+    const int b = blockIdx.y, c = threadIdx.x % LPR, slot = threadIdx.x / LPR;
     const int start = a.starts ? a.starts[(int64_t)b * a.st_s] : 0, count = a.counts[(int64_t)b * a.ct_s];
     const bool bad = start < 0 || count < 0 || count > a.N || (int64_t)start + count > (int64_t)a.capacity;
     if (bad && threadIdx.x == 0 && blockIdx.x == 0)
         atomicOr(a.status, TA_STATUS_BAD_SEQLEN);
-    const int end = bad ? a.N : count, groups = (end + a.tokens - 1) / a.tokens;
-    const int lpr = (a.D + PER - 1) / PER, rows_tok = 2 * a.Hkv;
+    const int end = bad ? a.N : count, groups = (end + a.tokens - 1) / a.tokens, rows_tok = 2 * a.Hkv;
     for (int grp = blockIdx.x; grp < groups; grp += gridDim.x) {
-        const int t0 = grp * a.tokens, n = min(a.tokens, end - t0), total = n * rows_tok * lpr;
-        for (int x = threadIdx.x; x < total; x += ROWS_THREADS) {
-            const int r = x / lpr, c = x - r * lpr, tok = r / rows_tok, y = r - tok * rows_tok;
+        const int t0 = grp * a.tokens, n = min(a.tokens, end - t0);
+        __syncthreads();                                   // the table of the group before is no longer read
+        if ((int)threadIdx.x < n) {
+            RowsPlace r = {b, start + t0 + (int)threadIdx.x};
+            if (bad) {
+                r.page = -1;
+            } else if (a.page_table) {
+                const int pos = start + t0 + (int)threadIdx.x, k = pos / a.ps;
+                r.page = a.page_table[(int64_t)b * a.pt_sb + k];
+                r.slot = pos - k * a.ps;
+                if (r.page < 0 || r.page >= a.n_pages) {
+                    r.page = -1;
+                    atomicOr(a.status, TA_STATUS_BAD_PAGE);
+                }
+            }
+            place[threadIdx.x] = r;
+        }
+        __syncthreads();
+        // (heads and tokens as in ta_rows_kernel)
+        for (int y0 = 0; y0 < rows_tok; y0 += RPP) {
+            const int m = min(RPP, rows_tok - y0), tpp = RPP / m, tok0 = slot / m, y = y0 + slot - tok0 * m;
             const bool is_v = y >= a.Hkv;
-            const int h = is_v ? y - a.Hkv : y, t = t0 + tok;
-            int64_t page = b, slot = (int64_t)start + t;
-            bool lost = bad;
-            if (!bad && a.page_table) {
-                const int pos = start + t, k = pos / a.ps;
-                page = a.page_table[(int64_t)b * a.pt_sb + k];
-                slot = pos - k * a.ps;
-                if (page < 0 || page >= a.n_pages) {
-                    lost = true;
-                    if (y == 0 && c == 0)
-                        atomicOr(a.status, TA_STATUS_BAD_PAGE);
-                }
-            }
-            float scale = __uint_as_float(0x7fc00000u);
-            uint32_t w[4] = {0u, 0u, 0u, 0u};
-            if (!lost) {
-                const char *src = is_v ? (const char *)a.vc + page * a.v_sp + (int64_t)h * a.v_sh + slot * a.v_ss
-                                       : (const char *)a.kc + page * a.k_sp + (int64_t)h * a.k_sh + slot * a.k_ss;
-                scale = q8_scale(is_v ? a.vs[page * a.vs_sp + (int64_t)h * a.vs_sh + slot * a.vs_ss]
-                                      : a.ks[page * a.ks_sp + (int64_t)h * a.ks_sh + slot * a.ks_ss]);
-                if (VEC) {
-                    const uint4 u = *(const uint4 *)(src + 16 * c);
-                    w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
-                } else {
-                    w[0] = ((const uint8_t *)src)[c];
-                }
-            }
-            char *dst = is_v ? (char *)a.v_out + ((int64_t)b * a.vo_sb + (int64_t)t * a.vo_st + (int64_t)h * a.vo_sh) * ES
-                             : (char *)a.k_out + ((int64_t)b * a.ko_sb + (int64_t)t * a.ko_st + (int64_t)h * a.ko_sh) * ES;
-            if (VEC) {
+            const int64_t h = is_v ? y - a.Hkv : y;
+            const char *src = is_v ? (const char *)a.vc + h * a.v_sh : (const char *)a.kc + h * a.k_sh;
+            const uint8_t *ssrc = is_v ? a.vs + h * a.vs_sh : a.ks + h * a.ks_sh;
+            char *dst = is_v ? (char *)a.v_out + (b * a.vo_sb + t0 * a.vo_st + h * a.vo_sh) * ES
+                             : (char *)a.k_out + (b * a.ko_sb + t0 * a.ko_st + h * a.ko_sh) * ES;
+            const int64_t sp = is_v ? a.v_sp : a.k_sp, ss = is_v ? a.v_ss : a.k_ss, ssp = is_v ? a.vs_sp : a.ks_sp,
+                          sss = is_v ? a.vs_ss : a.ks_ss, dst_st = (is_v ? a.vo_st : a.ko_st) * ES;
+            for (int c0 = c * PER; c0 < a.D && tok0 < tpp; c0 += LPR * PER)            // (once, but for single codes)
+                for (int tok1 = tok0; tok1 < n; tok1 += READ_AHEAD * tpp) {
+                    uint32_t w[READ_AHEAD][2], sb[READ_AHEAD];
 #pragma unroll
-                for (int i = 0; i < 4; i += BF16 ? 2 : 1) {
-                    float v[8];
-                    q8_values4(w[i], v);
-                    if (BF16) {
-                        q8_values4(w[i + 1], v + 4);
-                        *(uint4 *)(dst + 32 * c + 8 * i) =
-                            make_uint4(q8_pack_bf16(v[0] * scale, v[1] * scale), q8_pack_bf16(v[2] * scale, v[3] * scale),
-                                       q8_pack_bf16(v[4] * scale, v[5] * scale), q8_pack_bf16(v[6] * scale, v[7] * scale));
-                    } else {
-                        *(float4 *)(dst + 64 * c + 16 * i) = make_float4(v[0] * scale, v[1] * scale, v[2] * scale, v[3] * scale);
+                    for (int u = 0; u < READ_AHEAD; ++u) {
+                        const int tok = tok1 + u * tpp;
+                        w[u][0] = w[u][1] = 0u;
+                        sb[u] = 255u;
+                        if (tok < n && place[tok].page >= 0) {
+                            const RowsPlace at = place[tok];
+                            const char *from = src + at.page * sp + at.slot * ss + c0;
+                            sb[u] = ssrc[at.page * ssp + at.slot * sss];
+                            if (PER == 8) {
+                                const uint2 v = *(const uint2 *)from;
+                                w[u][0] = v.x;
+                                w[u][1] = v.y;
+                            } else {
+                                w[u][0] = PER == 4 ? *(const uint32_t *)from : (uint32_t) * (const uint8_t *)from;
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int u = 0; u < READ_AHEAD; ++u) {
+                        const int tok = tok1 + u * tpp;
+                        if (tok >= n)
+                            break;
+                        char *to = dst + tok * dst_st + c0 * ES;
+                        const float scale = q8_scale(sb[u]);
+                        float v[4];
+                        if (PER != 8)
+                            q8_values4(w[u][0], v);
+                        if (PER == 8)
+                            *(uint4 *)to = make_uint4(q8_bf16_2<false>(w[u][0], scale), q8_bf16_2<true>(w[u][0], scale),
+                                                      q8_bf16_2<false>(w[u][1], scale), q8_bf16_2<true>(w[u][1], scale));
+                        else if (PER == 4)
+                            *(float4 *)to = make_float4(v[0] * scale, v[1] * scale, v[2] * scale, v[3] * scale);
+                        else if (BF16)
+                            *(uint16_t *)to = (uint16_t)(q8_pack_bf16(v[0] * scale, 0.f) & 0xffffu);
+                        else
+                            *(float *)to = v[0] * scale;
                     }
                 }
-            } else if (BF16) {
-                ((uint16_t *)dst)[c] = (uint16_t)(q8_pack_bf16(q8_value(w[0]) * scale, 0.f) & 0xffffu);
-            } else {
-                ((float *)dst)[c] = q8_value(w[0]) * scale;
-            }
         }
     }
 }
 
-hipError_t ta_launch_q8_read(const TAQ8Read &r, hipStream_t stream)
+template <bool BF16>
+static hipError_t launch_read(const TAQ8Read &r, hipStream_t stream)
 {
+    constexpr int PER = BF16 ? 8 : 4;
+    if (r.tokens < 1 || r.tokens > READ_TOKENS)
+        return hipErrorInvalidValue;
     const int groups = (r.N + r.tokens - 1) / r.tokens;
     const dim3 grid(groups < 65536 ? groups : 65536, r.B), block(ROWS_THREADS);
-    if (r.vec && r.is_bf16)
-        hipLaunchKernelGGL((ta_q8_read_kernel<true, true>), grid, block, 0, stream, r);
-    else if (r.vec)
-        hipLaunchKernelGGL((ta_q8_read_kernel<false, true>), grid, block, 0, stream, r);
-    else if (r.is_bf16)
-        hipLaunchKernelGGL((ta_q8_read_kernel<true, false>), grid, block, 0, stream, r);
+    if (!r.vec)
+        hipLaunchKernelGGL((ta_q8_read_kernel<BF16, 1, TA_WAVE>), grid, block, 0, stream, r);
+    else if (r.D <= 64)
+        hipLaunchKernelGGL((ta_q8_read_kernel<BF16, PER, 64 / PER>), grid, block, 0, stream, r);
+    else if (r.D <= 128)
+        hipLaunchKernelGGL((ta_q8_read_kernel<BF16, PER, 128 / PER>), grid, block, 0, stream, r);
     else
-        hipLaunchKernelGGL((ta_q8_read_kernel<false, false>), grid, block, 0, stream, r);
+        hipLaunchKernelGGL((ta_q8_read_kernel<BF16, PER, 256 / PER>), grid, block, 0, stream, r);
     return hipGetLastError();
+}
+
+hipError_t ta_launch_q8_read(const TAQ8Read &r, hipStream_t stream)
+{
+    return r.is_bf16 ? launch_read<true>(r, stream) : launch_read<false>(r, stream);
 }
 
 // Bookkeeping after acceptance (see ta_compact_kernel): one workgroup per request; codes in pieces of type P, scales byte by byte.

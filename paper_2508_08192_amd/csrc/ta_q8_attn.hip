@@ -52,10 +52,8 @@ __device__ __forceinline__ uint32_t q8_row16_max(uint32_t x)           // over s
 // Eight codes times a power of two as bf16.
 __device__ __forceinline__ uint4 q8_bf16_8(int lo, int hi, float scale)
 {
-    return make_uint4(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false)),
-                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true)),
-                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false)),
-                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true)));
+    return make_uint4(q8_bf16_2<false>((uint32_t)lo, scale), q8_bf16_2<true>((uint32_t)lo, scale),
+                      q8_bf16_2<false>((uint32_t)hi, scale), q8_bf16_2<true>((uint32_t)hi, scale));
 }
 
 __device__ __forceinline__ void q8_lds_barrier()

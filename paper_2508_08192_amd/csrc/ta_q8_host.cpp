@@ -199,10 +199,10 @@ void set_cache(const ta_tensor *k, const ta_tensor *v, const ta_tensor *ks, cons
 
 // Tokens that a workgroup takes: one, until there are several workgroups per compute unit, whose start then counts more than
 // what one has to do (a prompt of 8000 tokens with 40 heads).
-int tokens_per_group(int64_t tokens_all, int64_t rows_per_token)
+int tokens_per_group(int64_t tokens_all, int64_t rows_per_token, int most = 8, int rows = 128)
 {
     int n = 1;
-    while (n < 8 && tokens_all / (2 * n) >= 4 * 256 && rows_per_token * n < 128)
+    while (n < most && tokens_all / (2 * n) >= 4 * 256 && rows_per_token * n < rows)
         n *= 2;
     return n;
 }
@@ -411,7 +411,7 @@ int ta_host_check_q8_read(const ta_tensor *k, const ta_tensor *v, const ta_tenso
     r->capacity = (int)c.capacity; r->n_pages = (int)c.n_pages;
     r->is_bf16 = ko->dtype == TA_BF16;
     r->vec = c.D % 16 == 0 && on_16_bytes(k) && on_16_bytes(v) && on_16_bytes(ko) && on_16_bytes(vo);
-    r->tokens = tokens_per_group(B * N, 2 * c.Hkv);
+    r->tokens = tokens_per_group(B * N, 2 * c.Hkv, 32, 512);
     return TA_OK;
 }
 
