@@ -402,7 +402,9 @@ int tree_attn_q8_fwd(const ta_tensor *q, const ta_tensor *k_cache, const ta_tens
     auto mark = [&](int i) { return !ev || !ev[i] || hipEventRecord((hipEvent_t)ev[i], st) == hipSuccess; };
     if (!mark(0))
         return TA_ERR_HIP;
-    if ((pr.plan.kernel == TA_KERNEL_MFMA ? ta_launch_q8_mfma(p, st, dev) : ta_launch_q8_generic(p, st, dev)) != hipSuccess || !mark(1))
+    const hipError_t e = pr.plan.kernel != TA_KERNEL_MFMA ? ta_launch_q8_generic(p, st, dev)
+                         : pr.p.basic ? ta_launch_q8_mfma(p, st, dev) : ta_launch_q8_tile(p, st, dev);
+    if (e != hipSuccess || !mark(1))
         return TA_ERR_HIP;
     if ((!p.solo && ta_launch_merge(p, st) != hipSuccess) || !mark(2))
         return TA_ERR_HIP;

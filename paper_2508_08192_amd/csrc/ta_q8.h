@@ -10,7 +10,7 @@ typedef unsigned short q8_u16x2 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ float q8_scale(uint32_t byte)               // 2^(byte - 127); 255: NaN
 {
-    return byte == 255u ? __uint_as_float(0x7fc00000u) : byte == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(byte << 23);
+    return __uint_as_float((byte << 23) | (((byte + 1u) & 255u) < 2u ? 0x00400000u : 0u));
 }
 
 // The scale byte of a row whose largest finite magnitude has the bits `top`: the smallest 2^e, e >= -126, with top <= 448 * 2^e
@@ -80,3 +80,4 @@ hipError_t ta_launch_q8_read(const TAQ8Read &r, hipStream_t stream);
 hipError_t ta_launch_q8_compact(const TAQ8Compact &c, hipStream_t stream);
 hipError_t ta_launch_q8_generic(const TAQ8Params &p, hipStream_t stream, int dev);
 hipError_t ta_launch_q8_mfma(const TAQ8Params &p, hipStream_t stream, int dev);
+hipError_t ta_launch_q8_tile(const TAQ8Params &p, hipStream_t stream, int dev);

@@ -1,6 +1,7 @@
 // Matrix-core KV pass over the 8-bit cache for gfx950: bf16 queries, head_dim 64 or 128, fp32 accumulation.
 //
-// As in the key-split kernel (ta_mfma_ks.hip) a workgroup keeps 32 RB query rows of one (request, KV head) and its waves split the
+// For up to 32 query rows of a (request, KV head); more of them go to ta_q8_tile.hip.  As in the key-split kernel
+// (ta_mfma_ks.hip) a workgroup keeps the rows and its waves split the
 // KEYS of its share: wave w takes every NW-th run of 32 tokens with its own running softmax, moves its own codes HBM -> LDS into a
 // ring that only it reads, and meets the others when the item ends.  What is different is the arithmetic, per 32 tokens:
 //
@@ -68,45 +69,42 @@ __device__ __forceinline__ void q8_vm_wait()
 }
 
 // Every lane moves 16 bytes from its global address to LDS lds_wave_base + 16 * lane (or a byte to a word of its own, 4 * lane).
+// (nt: nobody else reads what is loaded, and a stream that is read once passes by faster: one new token of 128 requests 116 us,
+// 122 without.)
+#define Q8_DMA(text, ...) asm volatile("s_mov_b32 m0, %[m]\n\ts_nop 0\n\t" text ::__VA_ARGS__ : "memory")
+
 __device__ __forceinline__ void q8_dma(const void *gptr, uint32_t lds_wave_base)
 {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" ::"v"(gptr), "s"(lds_wave_base)
-                 : "memory");
+    Q8_DMA("global_load_lds_dwordx4 %[a], off nt", [a] "v"(gptr), [m] "s"(lds_wave_base));
 }
 
 __device__ __forceinline__ void q8_dma_byte(const void *gptr, uint32_t lds_wave_base)
 {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_ubyte %0, off nt" ::"v"(gptr), "s"(lds_wave_base)
-                 : "memory");
+    Q8_DMA("global_load_lds_ubyte %[a], off nt", [a] "v"(gptr), [m] "s"(lds_wave_base));
 }
 
 __device__ __forceinline__ void q8_dma_s(const void *base, uint32_t off, uint32_t lds_wave_base)
 {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(off), "s"(base), "s"(lds_wave_base)
-                 : "memory");
+    Q8_DMA("global_load_lds_dwordx4 %[o], %[b] nt", [o] "v"(off), [b] "s"(base), [m] "s"(lds_wave_base));
 }
 
 // Two or four such loads in a row, 1 KB apart in memory and in LDS (the instruction's offset counts on both sides).
 __device__ __forceinline__ void q8_dma_2k(const void *base, uint32_t o0, uint32_t o1, uint32_t lds_wave_base)
 {
-    asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\t"
-                 "global_load_lds_dwordx4 %0, %2 nt\n\tglobal_load_lds_dwordx4 %1, %2 offset:1024 nt"
-                 ::"v"(o0), "v"(o1), "s"(base), "s"(lds_wave_base)
-                 : "memory");
+    Q8_DMA("global_load_lds_dwordx4 %[o], %[b] nt\n\tglobal_load_lds_dwordx4 %[p], %[b] offset:1024 nt",
+           [o] "v"(o0), [p] "v"(o1), [b] "s"(base), [m] "s"(lds_wave_base));
 }
 
 __device__ __forceinline__ void q8_dma_4k(const void *base, uint32_t o0, uint32_t o1, uint32_t lds_wave_base)
 {
-    asm volatile("s_mov_b32 m0, %3\n\ts_nop 0\n\t"
-                 "global_load_lds_dwordx4 %0, %2 nt\n\tglobal_load_lds_dwordx4 %1, %2 offset:1024 nt\n\t"
-                 "global_load_lds_dwordx4 %0, %2 offset:2048 nt\n\tglobal_load_lds_dwordx4 %1, %2 offset:3072 nt"
-                 ::"v"(o0), "v"(o1), "s"(base), "s"(lds_wave_base)
-                 : "memory");
+    Q8_DMA("global_load_lds_dwordx4 %[o], %[b] nt\n\tglobal_load_lds_dwordx4 %[p], %[b] offset:1024 nt\n\t"
+           "global_load_lds_dwordx4 %[o], %[b] offset:2048 nt\n\tglobal_load_lds_dwordx4 %[p], %[b] offset:3072 nt",
+           [o] "v"(o0), [p] "v"(o1), [b] "s"(base), [m] "s"(lds_wave_base));
 }
 
-// Sizes of one instance.  RB: 32-row blocks a wave keeps; NW: waves of a workgroup; OCC: workgroups per compute unit, which share
+// Sizes of one instance.  NW: waves of a workgroup; OCC: workgroups per compute unit, which share
 // its LDS.  A wave's ring holds NS runs of 32 tokens of K and as many of V; at the end it stages a block's fp32 results there.
-template <int DH, int RB, int NW, int OCC>
+template <int DH, int NW, int OCC>
 struct Q8Shape {
     static constexpr int ROW = DH;                         // bytes of a token row
     static constexpr int SUBB = Q8_SUB * ROW;              // bytes of 32 K (or V) rows
@@ -115,7 +113,7 @@ struct Q8Shape {
     static constexpr int NS = REGION / (2 * SUBB);         // runs in flight
     static constexpr int LD = SUBB / 1024;                 // 1 KB loads per run of K (or V)
     static constexpr int RPL = Q8_SUB / LD;                // token rows per load
-    static constexpr int ROWS = 32 * RB;
+    static constexpr int ROWS = 32;
     static constexpr int NT = 64 * NW;
     static constexpr int QB = ROWS * 2 * DH;               // bytes of the Q rows
     static constexpr int QP = (ROWS * DH / 8 + NT - 1) / NT;      // 16-byte pieces of bf16 rows a thread loads
@@ -128,19 +126,18 @@ struct Q8Shape {
 // p.solo).
 enum { Q8_CUT, Q8_SOLO };
 
-template <int DH, int RB, int NW, int OCC, int MODE>
+template <int DH, int NW, int OCC, int MODE>
 static constexpr size_t q8_smem(int B)
 {
-    return Q8Shape<DH, RB, NW, OCC>::FIXED + (MODE == Q8_SOLO || B <= TA_WAVE ? 0 : sizeof(int) * (B + 2 + (B <= Q8_LENS ? 2 * B : 0)));
+    return Q8Shape<DH, NW, OCC>::FIXED + (MODE == Q8_SOLO || B <= TA_WAVE ? 0 : sizeof(int) * (B + 2 + (B <= Q8_LENS ? 2 * B : 0)));
 }
 
-template <int DH, int RB, int NW, int OCC, int MODE>
+template <int DH, int NW, int OCC, int MODE>
 __global__ __launch_bounds__(64 * NW, OCC * NW / 4) void ta_q8_kv_kernel(TA_SCHED_PARAMS, TAQ8Params p)
 {
     const TASched sc = TA_SCHED;
-    using C = Q8Shape<DH, RB, NW, OCC>;
+    using C = Q8Shape<DH, NW, OCC>;
     constexpr bool SOLO = MODE == Q8_SOLO;
-    constexpr bool KEEP_Q = RB == 1 || DH == 64;                         // Q fragments stay in registers
     constexpr int NKK = DH / 16, NDB = DH / 32, SLOTS = DH / 16, QSLOTS = DH / 8;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     char *const qrows = smem + C::RING;                                 // Q rows of the item
@@ -152,7 +149,7 @@ __global__ __launch_bounds__(64 * NW, OCC * NW / 4) void ta_q8_kv_kernel(TA_SCHE
     const uint32_t lds0 = (uint32_t)(uintptr_t)((__attribute__((address_space(3))) char *)smem);
 
     const int tid = threadIdx.x, lane = tid & 63;
-    const int w = blockIdx.x, row0 = blockIdx.y * C::ROWS;               // first of the workgroup's query rows
+    const int w = blockIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r32 = lane & 31, hf = lane >> 5;
     // Schedule (see ta_build_schedule).  Up to 64 requests every wave keeps it in registers, lane b for request b: no
@@ -184,7 +181,6 @@ __global__ __launch_bounds__(64 * NW, OCC * NW / 4) void ta_q8_kv_kernel(TA_SCHE
         t = __builtin_amdgcn_readfirstlane(t);
         t_end = __builtin_amdgcn_readfirstlane(t_end);
     }
-    const int rows_here = min(C::ROWS, p.rows - row0);
     const float c = p.scale_log2e;
     const bool paged = p.page_table != nullptr;
     const uint32_t ksp = (uint32_t)p.k_sp, kss = (uint32_t)p.k_ss, vsp = (uint32_t)p.v_sp, vss = (uint32_t)p.v_ss;
@@ -311,7 +307,7 @@ __global__ __launch_bounds__(64 * NW, OCC * NW / 4) void ta_q8_kv_kernel(TA_SCHE
                 // rows past the group's end repeat its first row (their results are never stored)
                 const int x = i * C::NT + wave * 64 + l, row = x / QSLOTS;
                 if (C::ROWS * QSLOTS >= C::NT || row < C::ROWS) {
-                    const int R = row0 + (row < rows_here ? row : 0);
+                    const int R = row < p.rows ? row : 0;
                     const int node = (int)__umulhi((uint32_t)R << 8, p.g_magic);      // R / G
                     q_piece[i] = *(const uint4 *)((const uint16_t *)p.q + (int64_t)b * p.q_sb + (int64_t)node * p.q_st +
                                                (int64_t)(g * p.G + R - node * p.G) * p.q_sh + 8 * (x % QSLOTS));
@@ -348,15 +344,12 @@ __global__ __launch_bounds__(64 * NW, OCC * NW / 4) void ta_q8_kv_kernel(TA_SCHE
 
     bool more = next_item();
     while (more) {
-        q8_f32x16 o[RB][NDB];
-        float m_run[RB], l_run[RB];
-        unsigned long long tmask[RB];
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-            m_run[rb] = -INFINITY;
-            l_run[rb] = 0.f;
-            tmask[rb] = ~0ull;
-        }
+        q8_f32x16 o[NDB];
+        float m_run, l_run;
+        unsigned long long tmask;
+        m_run = -INFINITY;
+        l_run = 0.f;
+        tmask = ~0ull;
         const int u_last = last_own();
         int u = wave, pg_base = 0;
         // everything requested is here: no wait of the compiler for it may fall behind the loads into LDS, which it does
@@ -373,7 +366,7 @@ __global__ __launch_bounds__(64 * NW, OCC * NW / 4) void ta_q8_kv_kernel(TA_SCHE
             }
         }
 
-        // Loads of run u into ring slot sl: K part, LD loads of 1 KB and one of the scales, or V part, LD loads.
+        // Loads of run u into ring slot sl: K part, LD loads of 1 KB, or V part, one load of both scales and LD of 1 KB.
         auto issue = [&](int u, int sl, bool is_v) {
             const uint32_t dst = region + (is_v ? C::NS * C::SUBB : 0) + sl * C::SUBB;
             const uint32_t sdst = sregion + sl * 256;
@@ -386,6 +379,11 @@ __global__ __launch_bounds__(64 * NW, OCC * NW / 4) void ta_q8_kv_kernel(TA_SCHE
                 const uint32_t page0 = paged ? (uint32_t)__builtin_amdgcn_readlane(pg, pl) : (uint32_t)b;
                 const uint32_t page1 = ppr_shift ? (uint32_t)__builtin_amdgcn_readlane(pg, pl + 1) : page0;
                 const uint32_t sr0 = paged ? (uint32_t)(pos0 & (p.ps - 1)) : (uint32_t)pos0;
+                if (is_v) {
+                    const uint32_t page = r32 < 16 ? page0 : page1;
+                    const uint32_t sr = ppr_shift ? (uint32_t)(r32 & 15) : sr0 + (uint32_t)r32;
+                    q8_dma_byte(sgp + (uint64_t)page * ssp + (uint64_t)sr * sss, sdst);
+                }
                 if (dense) {
                     const char *base = (const char *)(gp + (uint64_t)page0 * sp + (uint64_t)sr0 * DH);
                     if constexpr (DH == 128)
@@ -401,11 +399,6 @@ __global__ __launch_bounds__(64 * NW, OCC * NW / 4) void ta_q8_kv_kernel(TA_SCHE
                         q8_dma_s(gp + (uint64_t)page * sp + (uint64_t)sr * ss, is_v ? voff[k % OFFS] : koff[k % OFFS], dst + k * 1024);
                     }
                 }
-                if (!is_v) {
-                    const uint32_t page = r32 < 16 ? page0 : page1;
-                    const uint32_t sr = ppr_shift ? (uint32_t)(r32 & 15) : sr0 + (uint32_t)r32;
-                    q8_dma_byte(sgp + (uint64_t)page * ssp + (uint64_t)sr * sss, sdst);
-                }
             } else {
                 // rows past the run's end and rows before the window start read an attended token of the run (their
                 // probabilities are exactly zero)
@@ -419,16 +412,16 @@ __global__ __launch_bounds__(64 * NW, OCC * NW / 4) void ta_q8_kv_kernel(TA_SCHE
                     sr = paged ? (uint32_t)(pos & (p.ps - 1)) : (uint32_t)pos;
                 };
                 uint32_t page, sr;
+                if (is_v) {
+                    place(r32, page, sr);
+                    q8_dma_byte(sgp + (uint64_t)page * ssp + (uint64_t)sr * sss, sdst);
+                }
 #pragma unroll
                 for (int k = 0; k < C::LD; ++k) {
                     const int row = k * C::RPL + lrow;
                     place(row, page, sr);
                     const int chunk = dslot ^ (is_v ? 2 * vx(row) : kx(row));
                     q8_dma(gp + (uint64_t)page * sp + (uint64_t)sr * ss + chunk * 16, dst + k * 1024);
-                }
-                if (!is_v) {
-                    place(r32, page, sr);
-                    q8_dma_byte(sgp + (uint64_t)page * ssp + (uint64_t)sr * sss, sdst);
                 }
             }
         };
@@ -450,24 +443,20 @@ __global__ __launch_bounds__(64 * NW, OCC * NW / 4) void ta_q8_kv_kernel(TA_SCHE
         // while the first runs are on their way: Q fragments into every wave's registers (one block of rows), O = 0 and, in a wave
         // that has tree tokens, the ancestor masks
         // (a lane's sixteen codes of a chunk are columns 32 j + 16 hf .. + 15: two products' worth, and Q's pieces go with them)
-        auto q_frag = [&](int rb, int kk) {
-            return *(const uint4 *)(qrows + (rb * 32 + r32) * 2 * DH + (((4 * (kk >> 1) + 2 * hf + (kk & 1)) ^ qx(r32)) << 4));
+        auto q_frag = [&](int kk) {
+            return *(const uint4 *)(qrows + r32 * 2 * DH + (((4 * (kk >> 1) + 2 * hf + (kk & 1)) ^ qx(r32)) << 4));
         };
-        uint4 qf[RB][NKK];
-        if (KEEP_Q && u < n_sub) {
+        uint4 qf[NKK];
+        if (u < n_sub) {
 #pragma unroll
-            for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-                for (int kk = 0; kk < NKK; ++kk)
-                    qf[rb][kk] = q_frag(rb, kk);
+            for (int kk = 0; kk < NKK; ++kk)
+                qf[kk] = q_frag(kk);
         }
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb)
+        for (int db = 0; db < NDB; ++db)
 #pragma unroll
-            for (int db = 0; db < NDB; ++db)
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    o[rb][db][i] = 0.f;
+            for (int i = 0; i < 16; ++i)
+                o[db][i] = 0.f;
         if (u_last < n_sub && u_last >= n_pre) {
             // lane i walks up from node i
             const int l = fresh_lane();
@@ -488,14 +477,11 @@ __global__ __launch_bounds__(64 * NW, OCC * NW / 4) void ta_q8_kv_kernel(TA_SCHE
             }
             if (__any(wrong))
                 bad |= TA_STATUS_BAD_PARENT;
-#pragma unroll
-            for (int rb = 0; rb < RB; ++rb) {
-                const int row = rb * 32 + (l & 31);
-                const int node = p.q_off + (int)__umulhi((uint32_t)(row0 + row) << 8, p.g_magic);
-                const uint32_t m_lo = __shfl((uint32_t)m, node & 63, TA_WAVE), m_hi = __shfl((uint32_t)(m >> 32), node & 63, TA_WAVE);
-                if (row < rows_here)
-                    tmask[rb] = ((unsigned long long)m_hi << 32) | m_lo;
-            }
+            const int row = (l & 31);
+            const int node = p.q_off + (int)__umulhi((uint32_t)row << 8, p.g_magic);
+            const uint32_t m_lo = __shfl((uint32_t)m, node & 63, TA_WAVE), m_hi = __shfl((uint32_t)(m >> 32), node & 63, TA_WAVE);
+            if (row < p.rows)
+                tmask = ((unsigned long long)m_hi << 32) | m_lo;
         }
 
         int sl = 0;
@@ -513,7 +499,7 @@ __global__ __launch_bounds__(64 * NW, OCC * NW / 4) void ta_q8_kv_kernel(TA_SCHE
                 q8_vm_wait<C::LD + RUN>();
             else
                 q8_vm_wait<C::LD>();
-            // ---- scales: a lane of the upper half turns the byte of its token into V's factor, and all lanes take those of their tokens
+            // ---- scales: a lane of the upper half turns the byte of its token into V's factor
             uint32_t *const ssl = sring + sl * 64;
             const int pos0 = sub_pos(u), cnt = sub_end(u) - pos0;
             const bool tree = u >= n_pre;
@@ -522,7 +508,7 @@ __global__ __launch_bounds__(64 * NW, OCC * NW / 4) void ta_q8_kv_kernel(TA_SCHE
             if (hf)
                 ssl[32 + r32] = __float_as_uint(q8_scale(own));
             // ---- S^T = K . Q^T
-            q8_f32x16 s[RB];
+            q8_f32x16 s;
             const char *kt = kring + sl * C::SUBB + kf_row;
 #pragma unroll
             for (int j = 0; j < NKK / 2; ++j) {
@@ -531,25 +517,12 @@ __global__ __launch_bounds__(64 * NW, OCC * NW / 4) void ta_q8_kv_kernel(TA_SCHE
                 for (int k2 = 0; k2 < 2; ++k2) {
                     const int kk = 2 * j + k2;
                     const uint4 kf = q8_bf16_8(k2 ? x.z : x.x, k2 ? x.w : x.y, ks);
-#pragma unroll
-                    for (int rb = 0; rb < RB; ++rb) {
-                        const q8_f32x16 z = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-                        const uint4 qk = KEEP_Q ? qf[rb][kk] : q_frag(rb, kk);
-                        s[rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(q8_bf16x8, kf), __builtin_bit_cast(q8_bf16x8, qk),
-                                                                        kk == 0 ? z : s[rb], 0, 0, 0);
-                    }
+                    const q8_f32x16 z = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(q8_bf16x8, kf), __builtin_bit_cast(q8_bf16x8, qf[kk]),
+                                                                kk == 0 ? z : s, 0, 0, 0);
                 }
             }
-            float vs[16];
-#pragma unroll
-            for (int i4 = 0; i4 < 4; ++i4) {
-                const uint4 x = *(const uint4 *)(ssl + 32 + 8 * i4 + 4 * hf);
-                vs[4 * i4] = __uint_as_float(x.x);
-                vs[4 * i4 + 1] = __uint_as_float(x.y);
-                vs[4 * i4 + 2] = __uint_as_float(x.z);
-                vs[4 * i4 + 3] = __uint_as_float(x.w);
-            }
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");             // K rows and scales are in registers: their slots are free
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");             // the K rows are in registers: their slot is free
             if (ahead) {
                 const int i = (un - wave) / NW - pg_base;
                 if (paged && (i << ppr_shift) >= TA_WAVE) {
@@ -559,53 +532,47 @@ __global__ __launch_bounds__(64 * NW, OCC * NW / 4) void ta_q8_kv_kernel(TA_SCHE
                 issue(un, sl, false);
             }
             // ---- scores of tokens that do not exist, or that are no ancestors, become -inf
-            uint32_t seen[RB];
+            uint32_t seen;
             const bool masked = tree || cnt < Q8_SUB || pos0 < S;
             if (masked) {
                 uint32_t vm = cnt < Q8_SUB ? (1u << cnt) - 1u : ~0u;
                 if (!tree && pos0 < S)
                     vm &= ~((1u << (S - pos0)) - 1u);
+                uint32_t mm = vm;
+                if (tree)
+                    mm &= (uint32_t)(tmask >> ((u - n_pre) * Q8_SUB));
+                seen = mm;
+                mm >>= 4 * hf;
 #pragma unroll
-                for (int rb = 0; rb < RB; ++rb) {
-                    uint32_t mm = vm;
-                    if (tree)
-                        mm &= (uint32_t)(tmask[rb] >> ((u - n_pre) * Q8_SUB));
-                    seen[rb] = mm;
-                    mm >>= 4 * hf;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (!((mm >> (8 * (i / 4) + (i % 4))) & 1u))
-                            s[rb][i] = -INFINITY;
-                }
+                for (int i = 0; i < 16; ++i)
+                    if (!((mm >> (8 * (i / 4) + (i % 4))) & 1u))
+                        s[i] = -INFINITY;
             }
             // ---- running softmax
+            float t0 = s[0], t1 = s[1], t2 = s[2], t3 = s[3];
 #pragma unroll
-            for (int rb = 0; rb < RB; ++rb) {
-                float t0 = s[rb][0], t1 = s[rb][1], t2 = s[rb][2], t3 = s[rb][3];
+            for (int i = 4; i < 16; i += 4) {
+                t0 = fmaxf(t0, s[i]);
+                t1 = fmaxf(t1, s[i + 1]);
+                t2 = fmaxf(t2, s[i + 2]);
+                t3 = fmaxf(t3, s[i + 3]);
+            }
+            const float top = fmaxf(fmaxf(t0, t1), fmaxf(t2, t3)) * c;           // of this lane's sixteen scores
+            // (the reference moves only when a score exceeds it by more than 2^4: see ta_mfma_ks.hip)
+            if (__any(top > m_run + (SOLO ? 0.f : 4.f))) {
+                const float m_new = fmaxf(m_run, q8_swap_max(top));
+                const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+                m_run = m_new;
+                l_run *= alpha;
 #pragma unroll
-                for (int i = 4; i < 16; i += 4) {
-                    t0 = fmaxf(t0, s[rb][i]);
-                    t1 = fmaxf(t1, s[rb][i + 1]);
-                    t2 = fmaxf(t2, s[rb][i + 2]);
-                    t3 = fmaxf(t3, s[rb][i + 3]);
-                }
-                const float top = fmaxf(fmaxf(t0, t1), fmaxf(t2, t3)) * c;           // of this lane's sixteen scores
-                // (the reference moves only when a score exceeds it by more than 2^4: see ta_mfma_ks.hip)
-                if (__any(top > m_run[rb] + (SOLO ? 0.f : 4.f))) {
-                    const float m_new = fmaxf(m_run[rb], q8_swap_max(top));
-                    const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run[rb] - m_new);
-                    m_run[rb] = m_new;
-                    l_run[rb] *= alpha;
+                for (int db = 0; db < NDB; ++db)
 #pragma unroll
-                    for (int db = 0; db < NDB; ++db)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            o[rb][db][i] *= alpha;
-                }
+                    for (int i = 0; i < 16; ++i)
+                        o[db][i] *= alpha;
             }
             // ---- V.  Younger than it: the runs behind, and the K part just requested
             if (ahead)
-                q8_vm_wait<(C::NS - 1) * RUN + C::LD + 1>();
+                q8_vm_wait<(C::NS - 1) * RUN + C::LD>();
             else if (later >= 3)
                 q8_vm_wait<3 * RUN>();
             else if (later == 2)
@@ -635,19 +602,15 @@ __global__ __launch_bounds__(64 * NW, OCC * NW / 4) void ta_q8_kv_kernel(TA_SCHE
                         half[k] = make_uint4(clear(x.x), clear(x.y), clear(x.z), clear(x.w));
                     }
                     const uint32_t tokens = (uint32_t)hit | (uint32_t)(hit >> 32);
+                    if (hf && q8_scale(own) != q8_scale(own))
+                        ssl[32 + r32] = 0u;
+                    if (seen & tokens) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (vs[i] != vs[i])
-                            vs[i] = 0.f;
+                        for (int db = 0; db < NDB; ++db)
 #pragma unroll
-                    for (int rb = 0; rb < RB; ++rb)
-                        if (seen[rb] & tokens) {
-#pragma unroll
-                            for (int db = 0; db < NDB; ++db)
-#pragma unroll
-                                for (int i = 0; i < 16; ++i)
-                                    o[rb][db][i] = __uint_as_float(0x7fc00000u);
-                        }
+                            for (int i = 0; i < 16; ++i)
+                                o[db][i] = __uint_as_float(0x7fc00000u);
+                    }
                     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
                 }
             }
@@ -661,35 +624,34 @@ __global__ __launch_bounds__(64 * NW, OCC * NW / 4) void ta_q8_kv_kernel(TA_SCHE
                     vf[kb][db] = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
                         (lds_i2)(vt + vf_row + kb * 16 * C::ROW + (((2 * db + vh16) ^ vf_x) << 4)));
             __builtin_amdgcn_sched_barrier(0);
-            uint4 pb[RB][2];
+            uint4 pb[2];
+            // (a row that has not seen a token yet keeps -inf: its probabilities are exp2(-inf) = 0)
+            const float neg_m = m_run == -INFINITY ? 0.f : -m_run;
+            float sum = 0.f;
+            uint32_t pk[8];
 #pragma unroll
-            for (int rb = 0; rb < RB; ++rb) {
-                // (a row that has not seen a token yet keeps -inf: its probabilities are exp2(-inf) = 0)
-                const float neg_m = m_run[rb] == -INFINITY ? 0.f : -m_run[rb];
-                float sum[2] = {0.f, 0.f};
-                uint32_t pk[8];
+            for (int i4 = 0; i4 < 4; ++i4) {
+                const uint4 vs = *(const uint4 *)(ssl + 32 + 8 * i4 + 4 * hf);       // V's factors of the lane's four tokens
+                float e[4];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float e0 = __builtin_amdgcn_exp2f(fmaf(s[rb][2 * i], c, neg_m));
-                    const float e1 = __builtin_amdgcn_exp2f(fmaf(s[rb][2 * i + 1], c, neg_m));
-                    sum[i & 1] += e0 + e1;
-                    pk[i] = q8_pack_bf16(e0 * vs[2 * i], e1 * vs[2 * i + 1]);
-                }
-                l_run[rb] += sum[0] + sum[1];
-                pb[rb][0] = make_uint4(pk[0], pk[1], pk[2], pk[3]);
-                pb[rb][1] = make_uint4(pk[4], pk[5], pk[6], pk[7]);
+                for (int i = 0; i < 4; ++i)
+                    e[i] = __builtin_amdgcn_exp2f(fmaf(s[4 * i4 + i], c, neg_m));
+                sum += (e[0] + e[1]) + (e[2] + e[3]);
+                pk[2 * i4] = q8_pack_bf16(e[0] * __uint_as_float(vs.x), e[1] * __uint_as_float(vs.y));
+                pk[2 * i4 + 1] = q8_pack_bf16(e[2] * __uint_as_float(vs.z), e[3] * __uint_as_float(vs.w));
             }
+            l_run += sum;
+            pb[0] = make_uint4(pk[0], pk[1], pk[2], pk[3]);
+            pb[1] = make_uint4(pk[4], pk[5], pk[6], pk[7]);
             // ---- O^T += V^T . P^T
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
                 for (int db = 0; db < NDB; ++db) {
                     const uint4 a = q8_bf16_8(vf[kb][db].x, vf[kb][db].y, 1.f);
-#pragma unroll
-                    for (int rb = 0; rb < RB; ++rb)
-                        o[rb][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(q8_bf16x8, a),
-                                                                            __builtin_bit_cast(q8_bf16x8, pb[rb][kb]),
-                                                                            o[rb][db], 0, 0, 0);
+                    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(q8_bf16x8, a),
+                                                                        __builtin_bit_cast(q8_bf16x8, pb[kb]),
+                                                                        o[db], 0, 0, 0);
                 }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");             // the V rows are in registers
             if (ahead)
@@ -709,136 +671,126 @@ __global__ __launch_bounds__(64 * NW, OCC * NW / 4) void ta_q8_kv_kernel(TA_SCHE
             }
             if (l_e == 0)
                 wbad[wave] = wb;
-#pragma unroll
-            for (int rb = 0; rb < RB; ++rb) {
-                const float l_tot = l_run[rb] + __shfl_xor(l_run[rb], 32, TA_WAVE);
-                if (hf_e == 0) {
-                    stat[(wave * 2 + 0) * C::ROWS + rb * 32 + r32_e] = m_run[rb];
-                    stat[(wave * 2 + 1) * C::ROWS + rb * 32 + r32_e] = l_tot;
-                }
+            const float l_tot = l_run + __shfl_xor(l_run, 32, TA_WAVE);
+            if (hf_e == 0) {
+                stat[(wave * 2 + 0) * C::ROWS + r32_e] = m_run;
+                stat[(wave * 2 + 1) * C::ROWS + r32_e] = l_tot;
             }
         }
         const int slot_e = slot, b_e = b, g_e = g;
+        if (wave < n_live) {                               // (nobody reads what the others would put there)
+            float *stage = (float *)(smem + wave * C::REGION);
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-            if (rb > 0)
-                q8_lds_barrier();                              // the block before has been read
-            if (wave < n_live) {                               // (nobody reads what the others would put there)
-                float *stage = (float *)(smem + wave * C::REGION);
+            for (int db = 0; db < NDB; ++db)
 #pragma unroll
-                for (int db = 0; db < NDB; ++db)
-#pragma unroll
-                    for (int i4 = 0; i4 < 4; ++i4) {
-                        const int ch = db * 8 + 2 * i4 + hf_e;
-                        *(float4 *)(stage + r32_e * DH + ((ch ^ (r32_e & 15)) << 2)) =
-                            make_float4(o[rb][db][4 * i4], o[rb][db][4 * i4 + 1], o[rb][db][4 * i4 + 2], o[rb][db][4 * i4 + 3]);
-                    }
-            }
-            if (rb == RB - 1)
-                more = next_item();                            // its requests are on their way during the rest
-            q8_lds_barrier();
-            int any_bad = 0;
-#pragma unroll
-            for (int k = 0; k < NW; ++k)
-                any_bad |= wbad[k];
-            const int x_e = wave * 64 + l_e;
-            constexpr int TPR = 16, CPT = DH / TPR;            // threads per row, columns per thread
-#pragma unroll 1
-            for (int rr = x_e / TPR; rr < 32; rr += C::NT / TPR) {
-                const int c0 = (x_e % TPR) * (CPT / 4), row = rb * 32 + rr;
-                float mw[NW], big = -INFINITY;
-#pragma unroll
-                for (int k = 0; k < NW; ++k) {
-                    mw[k] = stat[(k * 2 + 0) * C::ROWS + row];
-                    big = fmaxf(big, mw[k]);
+                for (int i4 = 0; i4 < 4; ++i4) {
+                    const int ch = db * 8 + 2 * i4 + hf_e;
+                    *(float4 *)(stage + r32_e * DH + ((ch ^ (r32_e & 15)) << 2)) =
+                        make_float4(o[db][4 * i4], o[db][4 * i4 + 1], o[db][4 * i4 + 2], o[db][4 * i4 + 3]);
                 }
-                float l_tot = 0.f, acc[CPT];
+        }
+        more = next_item();                                // its requests are on their way during the rest
+        q8_lds_barrier();
+        int any_bad = 0;
 #pragma unroll
-                for (int i = 0; i < CPT; ++i)
-                    acc[i] = 0.f;
+        for (int k = 0; k < NW; ++k)
+            any_bad |= wbad[k];
+        const int x_e = wave * 64 + l_e;
+        constexpr int TPR = 16, CPT = DH / TPR;            // threads per row, columns per thread
+#pragma unroll 1
+        for (int row = x_e / TPR; row < 32; row += C::NT / TPR) {
+            const int c0 = (x_e % TPR) * (CPT / 4);
+            float mw[NW], big = -INFINITY;
 #pragma unroll
-                for (int k0 = 0; k0 < NW; k0 += 4)
-                    if (k0 < n_live) {
+            for (int k = 0; k < NW; ++k) {
+                mw[k] = stat[(k * 2 + 0) * C::ROWS + row];
+                big = fmaxf(big, mw[k]);
+            }
+            float l_tot = 0.f, acc[CPT];
 #pragma unroll
-                        for (int k = k0; k < k0 + 4; ++k) {
-                            const float wgt = mw[k] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw[k] - big);
-                            l_tot = fmaf(wgt, stat[(k * 2 + 1) * C::ROWS + row], l_tot);
+            for (int i = 0; i < CPT; ++i)
+                acc[i] = 0.f;
 #pragma unroll
-                            for (int q = 0; q < CPT / 4; ++q) {
-                                const float4 x = *(const float4 *)(smem + k * C::REGION + (rr * DH + (((c0 + q) ^ (rr & 15)) << 2)) * 4);
-                                acc[4 * q + 0] = fmaf(wgt, x.x, acc[4 * q + 0]);
-                                acc[4 * q + 1] = fmaf(wgt, x.y, acc[4 * q + 1]);
-                                acc[4 * q + 2] = fmaf(wgt, x.z, acc[4 * q + 2]);
-                                acc[4 * q + 3] = fmaf(wgt, x.w, acc[4 * q + 3]);
-                            }
+            for (int k0 = 0; k0 < NW; k0 += 4)
+                if (k0 < n_live) {
+#pragma unroll
+                    for (int k = k0; k < k0 + 4; ++k) {
+                        const float wgt = mw[k] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw[k] - big);
+                        l_tot = fmaf(wgt, stat[(k * 2 + 1) * C::ROWS + row], l_tot);
+#pragma unroll
+                        for (int q = 0; q < CPT / 4; ++q) {
+                            const float4 x = *(const float4 *)(smem + k * C::REGION + (row * DH + (((c0 + q) ^ (row & 15)) << 2)) * 4);
+                            acc[4 * q + 0] = fmaf(wgt, x.x, acc[4 * q + 0]);
+                            acc[4 * q + 1] = fmaf(wgt, x.y, acc[4 * q + 1]);
+                            acc[4 * q + 2] = fmaf(wgt, x.z, acc[4 * q + 2]);
+                            acc[4 * q + 3] = fmaf(wgt, x.w, acc[4 * q + 3]);
                         }
                     }
-                const float inv = any_bad ? 0.f : 1.f / l_tot;
-                // largest magnitude of the row, as bits: those of a NaN are above all others
-                uint32_t top = 0;
-#pragma unroll
-                for (int i = 0; i < CPT; ++i) {
-                    acc[i] *= inv;
-                    top = max(top, __float_as_uint(acc[i]) & 0x7fffffffu);
                 }
-                top = q8_row16_max(top);
-                const bool nan_seen = top > 0x7f800000u;
-                const float amax = nan_seen ? 0.f : __uint_as_float(top);
-                const float lse2 = any_bad ? __uint_as_float(0x7fc00000u) : big + log2f(l_tot);
-                if constexpr (SOLO) {
-                    // no merge: the rows go out as they are, by its rules: a NaN or an infinity spoils its row (the 16-bit format
-                    // holds neither), and no score above -inf leaves no log-sum-exp either
-                    if (row < rows_here) {
-                        const int R = row0 + row, node = (int)__umulhi((uint32_t)R << 8, p.g_magic), h = g_e * p.G + R - node * p.G;
-                        const bool nan = any_bad || nan_seen || amax == INFINITY || lse2 != lse2;
-                        uint32_t *dst = (uint32_t *)((uint16_t *)p.out + (int64_t)b_e * p.o_sb + (int64_t)node * p.o_st +
-                                                     (int64_t)h * p.o_sh + 4 * c0);
+            const float inv = any_bad ? 0.f : 1.f / l_tot;
+            // largest magnitude of the row, as bits: those of a NaN are above all others
+            uint32_t top = 0;
 #pragma unroll
-                        for (int q = 0; q < CPT / 4; ++q)
-                            *(uint2 *)(dst + 2 * q) = nan ? make_uint2(0x7fc07fc0u, 0x7fc07fc0u)
-                                                          : make_uint2(q8_pack_bf16(acc[4 * q], acc[4 * q + 1]), q8_pack_bf16(acc[4 * q + 2], acc[4 * q + 3]));
-                        if (p.lse && x_e % TPR == 0)
-                            p.lse[(int64_t)b_e * p.lse_sb + (int64_t)h * p.lse_sh + (int64_t)node * p.lse_st] =
-                                lse2 == -INFINITY ? __uint_as_float(0x7fc00000u) : lse2 * 0.6931471805599453f;
-                    }
-                } else if (row < rows_here) {
-                    float scale, to_q;
-                    ta_q15_scale(amax, nan_seen, scale, to_q);
-                    const int64_t wrow = ta_ws_row(p, slot_e, 0, row0 + row);
-                    uint32_t *dst = (uint32_t *)(ta_part_row(p, wrow) + 8 * c0);
+            for (int i = 0; i < CPT; ++i) {
+                acc[i] *= inv;
+                top = max(top, __float_as_uint(acc[i]) & 0x7fffffffu);
+            }
+            top = q8_row16_max(top);
+            const bool nan_seen = top > 0x7f800000u;
+            const float amax = nan_seen ? 0.f : __uint_as_float(top);
+            const float lse2 = any_bad ? __uint_as_float(0x7fc00000u) : big + log2f(l_tot);
+            if constexpr (SOLO) {
+                // no merge: the rows go out as they are, by its rules: a NaN or an infinity spoils its row (the 16-bit format
+                // holds neither), and no score above -inf leaves no log-sum-exp either
+                if (row < p.rows) {
+                    const int R = row, node = (int)__umulhi((uint32_t)R << 8, p.g_magic), h = g_e * p.G + R - node * p.G;
+                    const bool nan = any_bad || nan_seen || amax == INFINITY || lse2 != lse2;
+                    uint32_t *dst = (uint32_t *)((uint16_t *)p.out + (int64_t)b_e * p.o_sb + (int64_t)node * p.o_st +
+                                                 (int64_t)h * p.o_sh + 4 * c0);
 #pragma unroll
                     for (int q = 0; q < CPT / 4; ++q)
-                        *(uint2 *)(dst + 2 * q) = make_uint2(ta_q15_pack(acc[4 * q], acc[4 * q + 1], to_q),
-                                                             ta_q15_pack(acc[4 * q + 2], acc[4 * q + 3], to_q));
-                    // (a NaN log-sum-exp poisons the row in the merge)
-                    if (x_e % TPR == 0)
-                        *(float2 *)&p.ws_lse[2 * wrow] = make_float2(lse2, scale);
+                        *(uint2 *)(dst + 2 * q) = nan ? make_uint2(0x7fc07fc0u, 0x7fc07fc0u)
+                                                      : make_uint2(q8_pack_bf16(acc[4 * q], acc[4 * q + 1]), q8_pack_bf16(acc[4 * q + 2], acc[4 * q + 3]));
+                    if (p.lse && x_e % TPR == 0)
+                        p.lse[(int64_t)b_e * p.lse_sb + (int64_t)h * p.lse_sh + (int64_t)node * p.lse_st] =
+                            lse2 == -INFINITY ? __uint_as_float(0x7fc00000u) : lse2 * 0.6931471805599453f;
                 }
+            } else if (row < p.rows) {
+                float scale, to_q;
+                ta_q15_scale(amax, nan_seen, scale, to_q);
+                const int64_t wrow = ta_ws_row(p, slot_e, 0, row);
+                uint32_t *dst = (uint32_t *)(ta_part_row(p, wrow) + 8 * c0);
+#pragma unroll
+                for (int q = 0; q < CPT / 4; ++q)
+                    *(uint2 *)(dst + 2 * q) = make_uint2(ta_q15_pack(acc[4 * q], acc[4 * q + 1], to_q),
+                                                         ta_q15_pack(acc[4 * q + 2], acc[4 * q + 3], to_q));
+                // (a NaN log-sum-exp poisons the row in the merge)
+                if (x_e % TPR == 0)
+                    *(float2 *)&p.ws_lse[2 * wrow] = make_float2(lse2, scale);
             }
-            if (any_bad && x_e == 0 && rb == 0)
-                ta_raise(p, any_bad);
         }
+        if (any_bad && x_e == 0)
+            ta_raise(p, any_bad);
         q8_lds_barrier();                                      // the rings are free for the next item
     }
 }
 
-template <int DH, int RB, int NW, int OCC, int MODE>
+template <int DH, int NW, int OCC, int MODE>
 static hipError_t launch_q8(const TAQ8Params &p, hipStream_t stream, int dev)
 {
-    const size_t smem = q8_smem<DH, RB, NW, OCC, MODE>(p.B);
-    static_assert(OCC * Q8Shape<DH, RB, NW, OCC>::FIXED <= 160 * 1024, "OCC workgroups per compute unit");
+    const size_t smem = q8_smem<DH, NW, OCC, MODE>(p.B);
+    static_assert(OCC * Q8Shape<DH, NW, OCC>::FIXED <= 160 * 1024, "OCC workgroups per compute unit");
     if (smem > 160 * 1024)
         return hipErrorInvalidValue;
     static bool attr_set[64] = {};      // per device and instance; setting it twice is harmless
     if (!attr_set[dev]) {
-        hipError_t e = hipFuncSetAttribute((const void *)ta_q8_kv_kernel<DH, RB, NW, OCC, MODE>,
+        hipError_t e = hipFuncSetAttribute((const void *)ta_q8_kv_kernel<DH, NW, OCC, MODE>,
                                            hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
         if (e != hipSuccess)
             return e;
         attr_set[dev] = true;
     }
-    hipLaunchKernelGGL((ta_q8_kv_kernel<DH, RB, NW, OCC, MODE>), dim3(MODE == Q8_SOLO ? p.B * p.Hkv : p.n_wg, (p.rows + 32 * RB - 1) / (32 * RB)),
-                       dim3(64 * NW), smem, stream, TA_SCHED_ARGS(p), p);
+    hipLaunchKernelGGL((ta_q8_kv_kernel<DH, NW, OCC, MODE>), dim3(MODE == Q8_SOLO ? p.B * p.Hkv : p.n_wg), dim3(64 * NW), smem, stream, TA_SCHED_ARGS(p), p);
     return hipGetLastError();
 }
 
@@ -846,15 +798,13 @@ hipError_t ta_launch_q8_mfma(const TAQ8Params &p, hipStream_t stream, int dev)
 {
     if (dev < 0 || dev >= 64)
         return hipErrorInvalidDevice;
-    if ((p.ks_rows != 32 && p.ks_rows != 64) || (!p.solo && p.rows_grp % p.ks_rows != 0) || !p.part_q15 || p.ls != 2 || !p.is_bf16 || p.direct)
+    if (p.ks_rows != 32 || p.rows > 32 || (!p.solo && p.rows_grp != 32) || !p.part_q15 || p.ls != 2 || !p.is_bf16 || p.direct)
         return hipErrorInvalidValue;
     auto rows = [&](auto dh) {
         constexpr int D = decltype(dh)::value;
-        if (p.solo == TA_SOLO_PAIR)
-            return p.ks_rows == 32 ? launch_q8<D, 1, 4, 2, Q8_SOLO>(p, stream, dev) : hipErrorInvalidValue;
         if (p.solo)
-            return p.ks_rows == 32 ? launch_q8<D, 1, 8, 1, Q8_SOLO>(p, stream, dev) : launch_q8<D, 2, 8, 1, Q8_SOLO>(p, stream, dev);
-        return p.ks_rows == 32 ? launch_q8<D, 1, 8, 1, Q8_CUT>(p, stream, dev) : launch_q8<D, 2, 8, 1, Q8_CUT>(p, stream, dev);
+            return p.solo == TA_SOLO_PAIR ? launch_q8<D, 4, 2, Q8_SOLO>(p, stream, dev) : launch_q8<D, 8, 1, Q8_SOLO>(p, stream, dev);
+        return launch_q8<D, 8, 1, Q8_CUT>(p, stream, dev);
     };
     if (p.D == 128)
         return rows(std::integral_constant<int, 128>{});

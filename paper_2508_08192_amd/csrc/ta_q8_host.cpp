@@ -217,8 +217,21 @@ int plan_mfma(const ta_tensor *out, const ta_opts *opts, int num_cus, TAProblem 
     const int64_t tiles_cap = lists * ((p.capacity - p.T + TA_TILE - 1) / TA_TILE + 1);
     pl.kernel = TA_KERNEL_MFMA;
     pl.threads = 512;
-    p.basic = 1;
-    p.ks_rows = pl.ks_rows = p.D == 64 && p.rows > 32 && p.B <= TA_SP_MAX_BATCH ? 64 : 32;   // (the schedule of more does not fit in LDS)
+    // Query rows of a workgroup.  Up to 32 have a kernel of their own (ta_q8_attn.hip: every wave for itself).  More of them
+    // take tiles of 64, 128 or 256 rows, those that cost least: a pass over the keys takes 107, 178 and 308, relative to one another
+    // (256 rows, 4 requests of 131072 tokens: 856, 712 and 617 us, and 961 in blocks of 32; 64 rows, 32 requests of 8192 tokens: 90, 113
+    // and 168 us, and 101).
+    const int sizes[3] = {64, 128, 256}, costs[3] = {107, 178, 308};
+    p.ks_rows = 32;
+    for (int64_t i = 0, least = INT64_MAX; p.rows > 32 && i < 3; ++i) {
+        const int64_t cost = (int64_t)((p.rows + sizes[i] - 1) / sizes[i]) * costs[i];
+        if (cost < least) {
+            least = cost;
+            p.ks_rows = sizes[i];
+        }
+    }
+    pl.ks_rows = p.ks_rows;
+    p.basic = p.ks_rows == 32;
     const int blocks = (p.rows + p.ks_rows - 1) / p.ks_rows;
     p.rows_grp = pl.rows_grp = blocks * p.ks_rows;
     p.n_rg = pl.n_rg = 1;
@@ -253,7 +266,7 @@ int plan_mfma(const ta_tensor *out, const ta_opts *opts, int num_cus, TAProblem 
     pr->ws_ls_off = ta_host_align_up(rows_total * p.D * 2, 256);
     pr->ws_bytes = pr->ws_o_bytes + pr->ws_lse_bytes + ta_host_align_up((size_t)lists * 2 * sizeof(int32_t), 256);
     if (num_splits == 0 && item_cost == 0 && lists > 0 && p.merge_kind != TA_MERGE_GENERAL && tiles_cap / lists <= 18)
-        p.solo = lists * blocks <= num_cus ? TA_SOLO_WIDE : p.ks_rows == 32 ? TA_SOLO_PAIR : 0;
+        p.solo = lists * blocks <= num_cus ? TA_SOLO_WIDE : p.basic ? TA_SOLO_PAIR : 0;
     if (p.solo)
         pl.merge_wgs = 0;
     return TA_OK;

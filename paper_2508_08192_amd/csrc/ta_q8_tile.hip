@@ -1,0 +1,626 @@
+// KV pass over the 8-bit cache for many query rows (gfx950): bf16 queries, head_dim 64 or 128, fp32 accumulation.
+//
+// A workgroup of eight waves keeps 32 RBW rows (64, 128 or 256) of one (request, KV head) and walks its share in tiles of 128 tokens.
+// The codes of a tile become bf16 values once per workgroup: every wave loads sixteen tokens' codes and scales into registers two
+// tiles ahead, turns them into values (scales and all: a power of two leaves them exact) on their way into LDS one tile ahead, and
+// then multiplies its 32 rows with its part of the tile that all have written: wave w has rows 32 (w % RBW) .. and, of each tile's
+// four runs of 32 tokens, those that are w / RBW modulo 8 / RBW.  Two tiles lie in LDS, one barrier per tile.
+//
+//     S^T[token, row] = K . Q^T ;  O^T[d, row] += V^T . P^T       (as in ta_mfma_ks.hip, on v_mfma_f32_32x32x16_bf16)
+//
+// Where every wave converts for itself (ta_q8_attn.hip) a run of 32 tokens costs it 64 conversions beside 16 products of 32 cycles,
+// and the loads' addresses on top.  The tokens of the tree follow the prefix without a gap, in the same tiles; a row's mask
+// is laid over the positions.
+//
+// Two waves share a SIMD, w and w + 4, and one of them converts before its products, the other behind them (606 us without, at the
+// size below).  What bounds it is the matrix cores and the exponentials' unit in turn: 256 rows, 4 requests of 131072 tokens, 8 KV heads
+// take 594 to 617 us, 890 to 925 TFLOP/s, where a square product of 8192 in bf16 reaches 1200.  Not faster: waves of 64 rows, which
+// read half as many bytes of K and V from LDS, but have no registers left for all of Q (657 us); two groups of waves
+// that take turns at the matrix cores, with a barrier at every turn (695 us).
+#include <type_traits>
+
+#include "ta_q8.h"
+
+typedef __bf16 qt_bf16x8 __attribute__((ext_vector_type(8)));
+typedef float qt_f32x16 __attribute__((ext_vector_type(16)));
+typedef short qt_s4 __attribute__((ext_vector_type(4)));
+typedef short qt_s8 __attribute__((ext_vector_type(8)));
+typedef uint32_t qt_u32x4 __attribute__((ext_vector_type(4)));
+
+#define QT_TILE 128
+#define QT_LENS 256                              // batches of up to this many requests keep their lengths in LDS
+
+__device__ __forceinline__ float qt_swap_max(float x)      // over the two lanes that share a query row
+{
+    auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+__device__ __forceinline__ uint32_t qt_row16_max(uint32_t x)           // over sixteen neighbouring lanes
+{
+    auto up = [&](uint32_t y) { x = y > x ? y : x; };
+    up((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xf, 0xf, false));     // lanes 1 0 3 2 of every four
+    up((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xf, 0xf, false));     // 2 3 0 1
+    up((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x141, 0xf, 0xf, false));    // mirrored within eight
+    up((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x128, 0xf, 0xf, false));    // rotated by eight within sixteen
+    return x;
+}
+
+__device__ __forceinline__ void qt_lds_barrier()           // (loads into registers stay in flight)
+{
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+template <int DH>
+struct QtShape {
+    static constexpr int ROW = 2 * DH;                     // bytes of a token row in LDS
+    static constexpr int TILE = QT_TILE * ROW;             // of a tile's K (or V)
+    static constexpr int BUF = 2 * TILE;
+    static constexpr int LPR = DH / 16;                    // lanes of a row as it is loaded
+    static constexpr int RPL = 64 / LPR;                   // rows of a load
+    static constexpr int NL = 16 / RPL;                    // loads of a wave's sixteen rows of K (or V)
+    static constexpr int STAGE = 32 * DH * 4;              // a wave's results at the end
+    static constexpr int FIXED = 2 * BUF + 4 * 8 * 2 * 32 + 4 * 8 + 8 + 8;
+    static_assert(8 * STAGE <= 2 * BUF, "results are staged in the tiles' place");
+};
+
+enum { QT_CUT, QT_SOLO };                                  // see ta_q8_attn.hip
+
+template <int DH, int MODE>
+static constexpr size_t qt_smem(int B)
+{
+    return QtShape<DH>::FIXED + (MODE == QT_SOLO || B <= TA_WAVE ? 0 : sizeof(int) * (B + 2 + (B <= QT_LENS ? 2 * B : 0)));
+}
+
+template <int DH, int RBW, int MODE>
+__global__ __launch_bounds__(512, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS, TAQ8Params p)
+{
+    const TASched sc = TA_SCHED;
+    using C = QtShape<DH>;
+    constexpr bool SOLO = MODE == QT_SOLO;
+    constexpr int KW = 8 / RBW, NR = 4 / KW;                             // waves that share rows, runs of a tile for each of them
+    constexpr int NKK = DH / 16, NDB = DH / 32, NL = C::NL, ROWS = 32 * RBW;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    float *const stat = (float *)(smem + 2 * C::BUF);                    // [8][2][32]: reference and sum
+    int *const wbad = (int *)(stat + 8 * 2 * 32);                        // [8]: TA_STATUS_* bits a wave has met
+    unsigned long long *const nan_nodes = (unsigned long long *)(wbad + 8);   // nodes whose values hold a NaN
+    int *const cum = (int *)(nan_nodes + 2);                             // more than 64 requests: [B + 1] schedule
+    int *const lens = cum + sc.B + 1, *const starts = lens + sc.B;       // and, up to QT_LENS, lengths and window starts
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int w = blockIdx.x, row0 = blockIdx.y * ROWS;                  // first of the workgroup's query rows
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int rb = wave % RBW, kg = wave / RBW;
+    const int r32 = lane & 31, hf = lane >> 5;
+    // schedule, as in ta_q8_attn.hip
+    const bool in_regs = sc.B <= TA_WAVE;
+    int s_len = 0, s_start = 0, s_units = 0, s_cum = 0, total;
+    int t, t_end;
+    if constexpr (SOLO) {
+        s_len = sc.seq_lens[(int64_t)(w / sc.Hkv) * sc.sl_s];
+        s_start = ta_kv_start(sc, w / sc.Hkv);
+        ta_touch_args<TAParams>(s_len);
+        t = 0;
+        t_end = 1;
+    } else {
+        if (in_regs) {
+            if (lane < sc.B) {
+                s_len = sc.seq_lens[(int64_t)lane * sc.sl_s];
+                s_start = ta_kv_start(sc, lane);
+            }
+            ta_touch_args<TAParams>();
+            if (lane < sc.B)
+                s_units = ta_list_tiles(sc, s_len, s_start) + sc.pad;
+            s_cum = ta_wave_scan(s_units);
+            total = sc.Hkv * __builtin_amdgcn_readlane(s_cum, 63);
+        } else {
+            total = sc.Hkv * ta_build_schedule(sc, cum, sc.B <= QT_LENS ? lens : nullptr, sc.B <= QT_LENS ? starts : nullptr);
+        }
+        ta_wg_range(sc, total, w, t, t_end);
+        t = __builtin_amdgcn_readfirstlane(t);
+        t_end = __builtin_amdgcn_readfirstlane(t_end);
+    }
+    const int rows_here = min(ROWS, p.rows - row0);
+    const float c = p.scale_log2e;
+    const bool paged = p.page_table != nullptr;
+    // 16-byte slots of a row in LDS: K slot s of row r holds chunk s ^ kx(r), V slot s chunk s ^ 2 vx(r) (see ta_mfma_ks.hip)
+    auto kx = [](int r) { return DH == 64 ? (r >> 1) & 7 : r & 15; };
+    auto vx = [](int r) { return DH == 64 ? 2 * ((r >> 1) & 1) + ((r >> 2) & 1) : 2 * (r & 3) + ((r >> 2) & 1); };
+    const int kf_at = r32 * C::ROW + ((hf ^ kx(r32)) << 4);
+    const int vtk = 4 * hf + ((lane >> 2) & 3);
+    const int vf_at = vtk * C::ROW + (lane & 3) * 8 + ((((lane >> 4) & 1) ^ vx(vtk)) << 5);
+    const int lrow = lane / C::LPR, lchunk = lane % C::LPR;              // as a lane loads: its row of a load's, its sixteen columns
+
+    // ---- the current item: list (b, g), tokens at positions [first, end) of the request, those from L on being the tree's
+    int b = -1, g = 0, slot = 0, L = 0, first = 0, end = 0, base = 0, n_t = 0, bad = 0;
+    auto next_item = [&]() {
+        while (t < t_end) {
+            int n_b, j0, j1, S;
+            if constexpr (SOLO) {
+                t = t_end;
+                b = w / sc.Hkv;
+                g = w - b * sc.Hkv;
+                L = s_len;
+                S = s_start;
+                n_b = ta_list_tiles(sc, L, S);
+                j0 = 0;
+                j1 = n_b;
+            } else {
+                int cum_b, cum_e;
+                if (in_regs) {
+                    b = __popcll(__ballot(sc.Hkv * s_cum <= t));
+                    cum_e = __builtin_amdgcn_readlane(s_cum, b);
+                    cum_b = cum_e - __builtin_amdgcn_readlane(s_units, b);
+                } else {
+                    if (b < 0)
+                        b = ta_find_request(sc, cum, t);
+                    else if ((int64_t)sc.Hkv * cum[b + 1] <= t)
+                        ++b;
+                    b = __builtin_amdgcn_readfirstlane(b);
+                    cum_b = __builtin_amdgcn_readfirstlane(cum[b]);
+                    cum_e = __builtin_amdgcn_readfirstlane(cum[b + 1]);
+                }
+                const int n_u = cum_e - cum_b;                          // schedule units of one list
+                g = (t - sc.Hkv * cum_b) / n_u;
+                const int seg_start = sc.Hkv * cum_b + g * n_u;
+                n_b = n_u - sc.pad;
+                j0 = t - seg_start;
+                j1 = min(n_b, t_end - seg_start);
+                if (j1 <= j0) {
+                    t = seg_start + n_u;                               // t lies in the list's trailing padding
+                    continue;
+                }
+                t = seg_start + (j1 == n_b ? n_u : j1);
+                slot = w + b * sc.Hkv + g;
+                ta_note_owner(p, b, g, w, j0, j1, n_b);
+                if (in_regs) {
+                    L = __builtin_amdgcn_readlane(s_len, b);
+                    S = __builtin_amdgcn_readlane(s_start, b);
+                } else {
+                    L = __builtin_amdgcn_readfirstlane(sc.B <= QT_LENS ? lens[b] : sc.seq_lens[(int64_t)b * sc.sl_s]);
+                    S = __builtin_amdgcn_readfirstlane(sc.B <= QT_LENS ? starts[b] : ta_kv_start(sc, b));
+                }
+            }
+            b = __builtin_amdgcn_readfirstlane(b);
+            g = __builtin_amdgcn_readfirstlane(g);
+            L = __builtin_amdgcn_readfirstlane(L);
+            S = __builtin_amdgcn_readfirstlane(S);
+            j0 = __builtin_amdgcn_readfirstlane(j0);
+            j1 = __builtin_amdgcn_readfirstlane(j1);
+            const bool ok = ta_request_ok(sc, L, S);
+            bad = ok ? 0 : TA_STATUS_BAD_SEQLEN;
+            const int tile0 = ok ? S / TA_TILE : 0;
+            const bool has_tree = j1 == n_b;
+            first = has_tree && j0 == n_b - 1 ? L : max((tile0 + j0) * TA_TILE, S);
+            end = has_tree ? L + sc.T : min((tile0 + j1) * TA_TILE, L);
+            base = first & ~31;
+            n_t = !ok ? 0 : (end - base + QT_TILE - 1) / QT_TILE;
+            return true;
+        }
+        return false;
+    };
+
+    struct Raw {                                           // a wave's sixteen tokens of a tile
+        qt_u32x4 k[NL], v[NL];
+        uint32_t ks[NL], vs[NL];
+    };
+
+    while (next_item()) {
+        // ---- what the start of an item needs: Q, the tree, page ids of this wave's tokens (lane l: tile pg_base + l)
+        int pg = 0, pg_base = 0;
+        auto load_pages = [&](int from) {
+            const int pos = base + (from + lane) * QT_TILE + 16 * wave;
+            const int at = min(max(pos, first), end - 1);
+            return p.page_table[(int64_t)b * p.pt_sb + (at >> p.ps_shift)];
+        };
+        auto checked = [&](int id) {                       // a page id as an address: one outside the cache is reported
+            if (!ta_page_ok(p, id)) {
+                bad |= TA_STATUS_BAD_PAGE;
+                id = 0;
+            }
+            return id;
+        };
+        unsigned long long tmask = ~0ull;
+        if (!bad && paged)
+            pg = load_pages(0);
+        uint4 qf[NKK];
+        {
+            // rows past the group's end repeat its first row (their results are never stored)
+            const int row = rb * 32 + r32, R = row0 + (row < rows_here ? row : 0);
+            const int node = (int)__umulhi((uint32_t)R << 8, p.g_magic);              // R / G
+            const uint16_t *q = (const uint16_t *)p.q + (int64_t)b * p.q_sb + (int64_t)node * p.q_st + (int64_t)(g * p.G + R - node * p.G) * p.q_sh;
+#pragma unroll
+            for (int kk = 0; kk < NKK; ++kk)
+                qf[kk] = *(const uint4 *)(q + 16 * kk + 8 * hf);
+        }
+        int parent = 0;
+        unsigned long long gmask = 0;
+        const bool tree_here = !bad && end > L;
+        if (tree_here && lane < sc.T) {
+            if (p.masks_in)
+                gmask = ta_given_mask(p, b, lane);
+            else
+                parent = p.parent[(int64_t)b * p.par_sb + lane];
+        }
+        if (!bad && paged)
+            pg = checked(pg);
+        const uint8_t *const kgp = (const uint8_t *)p.k + (int64_t)g * p.k_sh, *const vgp = (const uint8_t *)p.v + (int64_t)g * p.v_sh;
+        const uint8_t *const ksp = p.ks + (int64_t)g * p.ks_sh, *const vsp = p.vs + (int64_t)g * p.vs_sh;
+
+        auto load_tile = [&](int j, Raw &x) {
+            if (j >= n_t)
+                return;
+            if (paged && j - pg_base >= TA_WAVE) {
+                pg_base = j;                                           // (waits)
+                pg = checked(load_pages(pg_base));
+            }
+            const int pos0 = base + j * QT_TILE + 16 * wave;
+            const uint32_t page = (uint32_t)__builtin_amdgcn_readlane(paged ? pg : b, paged ? j - pg_base : 0);
+            const uint32_t sl0 = (uint32_t)(paged ? pos0 & (p.ps - 1) : pos0);
+            // (bases are scalars, and the lanes' offsets fit in 32 bits: the host has seen to it)
+            const uint8_t *kb = kgp + (uint64_t)page * (uint32_t)p.k_sp + (uint64_t)sl0 * (uint32_t)p.k_ss;
+            const uint8_t *vb = vgp + (uint64_t)page * (uint32_t)p.v_sp + (uint64_t)sl0 * (uint32_t)p.v_ss;
+            const uint8_t *ksb = ksp + (uint64_t)page * (uint32_t)p.ks_sp + (uint64_t)sl0 * (uint32_t)p.ks_ss;
+            const uint8_t *vsb = vsp + (uint64_t)page * (uint32_t)p.vs_sp + (uint64_t)sl0 * (uint32_t)p.vs_ss;
+#pragma unroll
+            for (int i = 0; i < NL; ++i)
+                if (pos0 + i * C::RPL < end && pos0 + (i + 1) * C::RPL > first) {      // any token of these: their page is one of the request's
+                    // (rows past the last token are read as that one: a contiguous cache may end there)
+                    const uint32_t r = (uint32_t)(i * C::RPL + min(lrow, end - 1 - (pos0 + i * C::RPL)));
+                    x.k[i] = __builtin_nontemporal_load((const qt_u32x4 *)(kb + r * (uint32_t)p.k_ss + 16 * lchunk));
+                    x.v[i] = __builtin_nontemporal_load((const qt_u32x4 *)(vb + r * (uint32_t)p.v_ss + 16 * lchunk));
+                    x.ks[i] = ksb[r * (uint32_t)p.ks_ss];
+                    x.vs[i] = vsb[r * (uint32_t)p.vs_ss];
+                }
+        };
+        auto write_tile = [&](int j, Raw &x) {
+            if (j >= n_t)
+                return;
+            char *const kt = smem + (j & 1) * C::BUF, *const vt = kt + C::TILE;
+            const int pos0 = base + j * QT_TILE + 16 * wave;
+            const bool edge = pos0 < first || pos0 + 16 > min(L, end);
+#pragma unroll
+            for (int i = 0; i < NL; ++i) {
+                const int row = 16 * wave + i * C::RPL + lrow;
+                qt_u32x4 k = x.k[i], v = x.v[i];
+                uint32_t ks = x.ks[i], vs = x.vs[i];
+                if (edge) {
+                    // tokens of others are zeros; a NaN among a node's values counts only for rows that attend to it, so it is noted
+                    // and taken out of the product
+                    const int pos = pos0 + i * C::RPL + lrow;
+                    const bool mine = pos >= first && pos < end;
+                    if (!mine) {
+                        k = qt_u32x4{0u, 0u, 0u, 0u};
+                        ks = 127u;
+                    }
+                    uint32_t nan = vs == 255u ? 1u : 0u;
+#pragma unroll
+                    for (int n = 0; n < 4; ++n)
+                        nan |= ((v[n] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+                    if (mine && pos >= L && nan)
+                        atomicOr(nan_nodes, 1ull << (pos - L));
+                    if (!mine || (pos >= L && nan)) {
+                        v = qt_u32x4{0u, 0u, 0u, 0u};
+                        vs = 127u;
+                    }
+                }
+                const float kscale = q8_scale(ks), vscale = q8_scale(vs);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    *(uint4 *)(kt + row * C::ROW + (((2 * lchunk + h) ^ kx(row)) << 4)) =
+                        make_uint4(q8_bf16_2<false>(k[2 * h], kscale), q8_bf16_2<true>(k[2 * h], kscale),
+                                   q8_bf16_2<false>(k[2 * h + 1], kscale), q8_bf16_2<true>(k[2 * h + 1], kscale));
+                    *(uint4 *)(vt + row * C::ROW + (((2 * lchunk + h) ^ (2 * vx(row))) << 4)) =
+                        make_uint4(q8_bf16_2<false>(v[2 * h], vscale), q8_bf16_2<true>(v[2 * h], vscale),
+                                   q8_bf16_2<false>(v[2 * h + 1], vscale), q8_bf16_2<true>(v[2 * h + 1], vscale));
+                }
+            }
+        };
+
+        Raw even = {}, odd = {};
+        load_tile(0, even);
+        load_tile(1, odd);
+        if (tid == 0)
+            *nan_nodes = 0ull;
+        qt_f32x16 o[NDB];
+#pragma unroll
+        for (int db = 0; db < NDB; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                o[db][i] = 0.f;
+        float m_run = -INFINITY, l_run = 0.f;
+        if (tree_here) {
+            // lane i walks up from node i
+            unsigned long long m = 0;
+            bool wrong = false;
+            if (p.masks_in) {
+                m = gmask;
+                wrong = lane < sc.T && !ta_given_mask_ok(m, lane);
+            } else {
+                int cur = lane < sc.T ? lane : -1;
+                for (int steps = 0; __any(cur >= 0); ++steps) {
+                    wrong |= cur >= 0 && (cur >= sc.T || steps >= sc.T);
+                    if (cur >= 0)
+                        m |= 1ull << (cur & 63);
+                    const int up = __shfl(parent, cur & 63, TA_WAVE);
+                    cur = cur >= 0 && !wrong ? up : -1;
+                }
+            }
+            if (__any(wrong))
+                bad |= TA_STATUS_BAD_PARENT;
+            const int row = rb * 32 + r32, node = p.q_off + (int)__umulhi((uint32_t)(row0 + row) << 8, p.g_magic);
+            const uint32_t m_lo = __shfl((uint32_t)m, node & 63, TA_WAVE), m_hi = __shfl((uint32_t)(m >> 32), node & 63, TA_WAVE);
+            if (row < rows_here)
+                tmask = ((unsigned long long)m_hi << 32) | m_lo;
+        }
+        qt_lds_barrier();                                  // (nan_nodes is zero, and the tiles' place is free)
+        write_tile(0, even);
+        load_tile(2, even);
+        qt_lds_barrier();
+
+        // 32 tokens from position pos0 on, at row `at` of the tile in LDS
+        auto run = [&](int tile, int at, int pos0) {
+            // ---- S^T = K . Q^T
+            qt_f32x16 s = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            int ka = tile + at * C::ROW + kf_at, va = tile + C::TILE + at * C::ROW + vf_at;
+            asm volatile("" : "+v"(ka), "+v"(va));         // (one operation per address, where addresses that are kept would not fit in registers)
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+            for (int kk = 0; kk < NKK; ++kk) {
+                const uint4 kf = *(const uint4 *)(smem + (ka ^ (kk << 5)));
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(qt_bf16x8, kf), __builtin_bit_cast(qt_bf16x8, qf[kk]), s, 0, 0, 0);
+            }
+            // ---- V fragments: the first half is requested here and arrives under the softmax, the second under the products of the first
+            typedef __attribute__((address_space(3))) qt_s4 *lds_s4;
+            auto v_frag = [&](int kb, int db) {
+                const char *a = smem + (va ^ (db << 6)) + kb * 16 * C::ROW;
+                const qt_s4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)a);
+                const qt_s4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(a + 8 * C::ROW));
+                return __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
+            };
+            qt_s8 vf[NDB];
+#pragma unroll
+            for (int db = 0; db < NDB; ++db)
+                vf[db] = v_frag(0, db);
+            __builtin_amdgcn_s_setprio(0);
+            // ---- scores of tokens that do not exist, or that are no ancestors, become -inf
+            if (pos0 < first || pos0 + 32 > min(L, end)) {
+                uint32_t mm = 0;
+                if (pos0 < L) {
+                    const int n = min(L, end) - pos0;                  // prefix tokens from pos0 on
+                    mm = n >= 32 ? ~0u : n > 0 ? (1u << n) - 1u : 0u;
+                    if (pos0 < first)
+                        mm &= first - pos0 >= 32 ? 0u : ~((1u << (first - pos0)) - 1u);
+                }
+                if (end > L) {
+                    const unsigned long long tm = sc.T >= 64 ? tmask : tmask & ((1ull << sc.T) - 1ull);
+                    const int up = L - pos0;
+                    mm |= up >= 32 ? 0u : up >= 0 ? (uint32_t)tm << up : (uint32_t)(tm >> -up);
+                }
+                mm >>= 4 * hf;
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (!((mm >> (8 * (i / 4) + (i % 4))) & 1u))
+                        s[i] = -INFINITY;
+            }
+            // ---- running softmax (the reference moves only when a score exceeds it by more than 2^4: see ta_mfma_ks.hip)
+            float t0 = s[0], t1 = s[1], t2 = s[2], t3 = s[3];
+#pragma unroll
+            for (int i = 4; i < 16; i += 4) {
+                t0 = fmaxf(t0, s[i]);
+                t1 = fmaxf(t1, s[i + 1]);
+                t2 = fmaxf(t2, s[i + 2]);
+                t3 = fmaxf(t3, s[i + 3]);
+            }
+            const float top = fmaxf(fmaxf(t0, t1), fmaxf(t2, t3)) * c;
+            if (__any(top > m_run + (SOLO ? 0.f : 4.f))) {
+                const float m_new = fmaxf(m_run, qt_swap_max(top));
+                const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+                m_run = m_new;
+                l_run *= alpha;
+#pragma unroll
+                for (int db = 0; db < NDB; ++db)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        o[db][i] *= alpha;
+            }
+            const float neg_m = m_run == -INFINITY ? 0.f : -m_run;
+            uint32_t pk[8];
+            float sum[2] = {0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float e0 = __builtin_amdgcn_exp2f(fmaf(s[2 * i], c, neg_m)), e1 = __builtin_amdgcn_exp2f(fmaf(s[2 * i + 1], c, neg_m));
+                sum[i & 1] += e0 + e1;
+                pk[i] = q8_pack_bf16(e0, e1);
+            }
+            l_run += sum[0] + sum[1];
+            // ---- O^T += V^T . P^T
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+                const uint4 pb = make_uint4(pk[4 * kb], pk[4 * kb + 1], pk[4 * kb + 2], pk[4 * kb + 3]);
+#pragma unroll
+                for (int db = 0; db < NDB; ++db) {
+                    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(qt_bf16x8, vf[db]), __builtin_bit_cast(qt_bf16x8, pb),
+                                                                    o[db], 0, 0, 0);
+                    if (kb == 0)
+                        vf[db] = v_frag(1, db);
+                }
+            }
+            __builtin_amdgcn_s_setprio(0);
+        };
+        auto step = [&](int j, Raw &next) {
+            if (wave < 4) {
+                write_tile(j + 1, next);
+                load_tile(j + 3, next);
+            }
+            const int tile = (j & 1) * C::BUF;
+#pragma unroll 1
+            for (int r = 0; r < NR; ++r) {
+                const int at = 32 * (kg + KW * r), pos0 = base + j * QT_TILE + at;
+                if (pos0 < end && pos0 + 32 > first)
+                    run(tile, at, pos0);
+            }
+            if (wave >= 4) {
+                write_tile(j + 1, next);
+                load_tile(j + 3, next);
+            }
+            qt_lds_barrier();
+        };
+#pragma unroll 1
+        for (int j = 0; j < n_t; j += 2) {
+            step(j, odd);
+            if (j + 1 < n_t)
+                step(j + 1, even);
+        }
+
+        // ---- results: each wave stages its 32 x DH block (16-byte chunk ch of row r at chunk ch ^ (r & 15)), then the threads add up
+        // those of the waves that share rows
+        {
+            int wb = 0;
+            if (__any(bad)) {
+                for (int bit : {TA_STATUS_BAD_PARENT, TA_STATUS_BAD_SEQLEN, TA_STATUS_BAD_PAGE})
+                    wb |= __any(bad & bit) ? bit : 0;
+            }
+            if (lane == 0)
+                wbad[wave] = wb;
+            if (tree_here && (tmask & *nan_nodes)) {
+#pragma unroll
+                for (int db = 0; db < NDB; ++db)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        o[db][i] = __uint_as_float(0x7fc00000u);
+            }
+            const float l_tot = l_run + __shfl_xor(l_run, 32, TA_WAVE);
+            if (hf == 0) {
+                stat[(wave * 2 + 0) * 32 + r32] = m_run;
+                stat[(wave * 2 + 1) * 32 + r32] = l_tot;
+            }
+            float *stage = (float *)(smem + wave * C::STAGE);
+#pragma unroll
+            for (int db = 0; db < NDB; ++db)
+#pragma unroll
+                for (int i4 = 0; i4 < 4; ++i4) {
+                    const int ch = db * 8 + 2 * i4 + hf;
+                    *(float4 *)(stage + r32 * DH + ((ch ^ (r32 & 15)) << 2)) =
+                        make_float4(o[db][4 * i4], o[db][4 * i4 + 1], o[db][4 * i4 + 2], o[db][4 * i4 + 3]);
+                }
+        }
+        qt_lds_barrier();
+        int any_bad = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            any_bad |= wbad[k];
+        constexpr int CPT = DH / 16;                       // columns of a thread: sixteen of them per row
+#pragma unroll 1
+        for (int row = tid / 16; row < ROWS; row += 32) {
+            const int c0 = (tid % 16) * (CPT / 4), rr = row & 31, wv0 = row / 32;
+            float mw[KW], big = -INFINITY;
+#pragma unroll
+            for (int k = 0; k < KW; ++k) {
+                mw[k] = stat[((wv0 + k * RBW) * 2 + 0) * 32 + rr];
+                big = fmaxf(big, mw[k]);
+            }
+            float l_tot = 0.f, acc[CPT];
+#pragma unroll
+            for (int i = 0; i < CPT; ++i)
+                acc[i] = 0.f;
+#pragma unroll
+            for (int k = 0; k < KW; ++k) {
+                const float wgt = mw[k] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw[k] - big);
+                l_tot = fmaf(wgt, stat[((wv0 + k * RBW) * 2 + 1) * 32 + rr], l_tot);
+#pragma unroll
+                for (int q = 0; q < CPT / 4; ++q) {
+                    const float4 x = *(const float4 *)(smem + (wv0 + k * RBW) * C::STAGE + (rr * DH + (((c0 + q) ^ (rr & 15)) << 2)) * 4);
+                    acc[4 * q + 0] = fmaf(wgt, x.x, acc[4 * q + 0]);
+                    acc[4 * q + 1] = fmaf(wgt, x.y, acc[4 * q + 1]);
+                    acc[4 * q + 2] = fmaf(wgt, x.z, acc[4 * q + 2]);
+                    acc[4 * q + 3] = fmaf(wgt, x.w, acc[4 * q + 3]);
+                }
+            }
+            const float inv = any_bad ? 0.f : 1.f / l_tot;
+            // largest magnitude of the row, as bits: those of a NaN are above all others
+            uint32_t top = 0;
+#pragma unroll
+            for (int i = 0; i < CPT; ++i) {
+                acc[i] *= inv;
+                top = max(top, __float_as_uint(acc[i]) & 0x7fffffffu);
+            }
+            top = qt_row16_max(top);
+            const bool nan_seen = top > 0x7f800000u;
+            const float amax = nan_seen ? 0.f : __uint_as_float(top);
+            const float lse2 = any_bad ? __uint_as_float(0x7fc00000u) : big + log2f(l_tot);
+            if (row < rows_here) {
+                if constexpr (SOLO) {
+                    // (no merge: the rules are those of ta_q8_attn.hip)
+                    const int R = row0 + row, node = (int)__umulhi((uint32_t)R << 8, p.g_magic), h = g * p.G + R - node * p.G;
+                    const bool nan = any_bad || nan_seen || amax == INFINITY || lse2 != lse2;
+                    uint32_t *dst = (uint32_t *)((uint16_t *)p.out + (int64_t)b * p.o_sb + (int64_t)node * p.o_st + (int64_t)h * p.o_sh + 4 * c0);
+#pragma unroll
+                    for (int q = 0; q < CPT / 4; ++q)
+                        *(uint2 *)(dst + 2 * q) = nan ? make_uint2(0x7fc07fc0u, 0x7fc07fc0u)
+                                                      : make_uint2(q8_pack_bf16(acc[4 * q], acc[4 * q + 1]), q8_pack_bf16(acc[4 * q + 2], acc[4 * q + 3]));
+                    if (p.lse && tid % 16 == 0)
+                        p.lse[(int64_t)b * p.lse_sb + (int64_t)h * p.lse_sh + (int64_t)node * p.lse_st] =
+                            lse2 == -INFINITY ? __uint_as_float(0x7fc00000u) : lse2 * 0.6931471805599453f;
+                } else {
+                    float scale, to_q;
+                    ta_q15_scale(amax, nan_seen, scale, to_q);
+                    const int64_t wrow = ta_ws_row(p, slot, 0, row0 + row);
+                    uint32_t *dst = (uint32_t *)(ta_part_row(p, wrow) + 8 * c0);
+#pragma unroll
+                    for (int q = 0; q < CPT / 4; ++q)
+                        *(uint2 *)(dst + 2 * q) = make_uint2(ta_q15_pack(acc[4 * q], acc[4 * q + 1], to_q),
+                                                             ta_q15_pack(acc[4 * q + 2], acc[4 * q + 3], to_q));
+                    // (a NaN log-sum-exp poisons the row in the merge)
+                    if (tid % 16 == 0)
+                        *(float2 *)&p.ws_lse[2 * wrow] = make_float2(lse2, scale);
+                }
+            }
+        }
+        if (any_bad && tid == 0)
+            ta_raise(p, any_bad);
+        qt_lds_barrier();                                  // everything has been read
+    }
+}
+
+template <int DH, int RBW, int MODE>
+static hipError_t launch_tile(const TAQ8Params &p, hipStream_t stream, int dev)
+{
+    const size_t smem = qt_smem<DH, MODE>(p.B);
+    static_assert(qt_smem<DH, MODE>(TA_MAX_BATCH) <= 160 * 1024, "whatever the batch");
+    static bool attr_set[64] = {};      // per device and instance; setting it twice is harmless
+    if (!attr_set[dev]) {
+        hipError_t e = hipFuncSetAttribute((const void *)ta_q8_tile_kernel<DH, RBW, MODE>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                           160 * 1024);
+        if (e != hipSuccess)
+            return e;
+        attr_set[dev] = true;
+    }
+    hipLaunchKernelGGL((ta_q8_tile_kernel<DH, RBW, MODE>), dim3(MODE == QT_SOLO ? p.B * p.Hkv : p.n_wg, (p.rows + 32 * RBW - 1) / (32 * RBW)),
+                       dim3(512), smem, stream, TA_SCHED_ARGS(p), p);
+    return hipGetLastError();
+}
+
+hipError_t ta_launch_q8_tile(const TAQ8Params &p, hipStream_t stream, int dev)
+{
+    if (dev < 0 || dev >= 64)
+        return hipErrorInvalidDevice;
+    if (!p.part_q15 || p.ls != 2 || !p.is_bf16 || p.direct || (!p.solo && p.rows_grp % p.ks_rows != 0))
+        return hipErrorInvalidValue;
+    auto with = [&](auto dh, auto rbw) {
+        constexpr int D = decltype(dh)::value, W = decltype(rbw)::value;
+        return p.solo ? launch_tile<D, W, QT_SOLO>(p, stream, dev) : launch_tile<D, W, QT_CUT>(p, stream, dev);
+    };
+    auto rows = [&](auto dh) {
+        switch (p.ks_rows) {
+        case 64: return with(dh, std::integral_constant<int, 2>{});
+        case 128: return with(dh, std::integral_constant<int, 4>{});
+        case 256: return with(dh, std::integral_constant<int, 8>{});
+        default: return hipErrorInvalidValue;
+        }
+    };
+    if (p.D == 128)
+        return rows(std::integral_constant<int, 128>{});
+    return p.D == 64 ? rows(std::integral_constant<int, 64>{}) : hipErrorInvalidValue;
+}
