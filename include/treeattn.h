@@ -437,8 +437,8 @@ int tree_attn_q8_compact(ta_tensor *k_cache, ta_tensor *v_cache, ta_tensor *k_sc
  * workspace and the errors as there.  Scores and outputs are those of the values code * scale, which are used as they are:
  * q is not rounded, bf16 probabilities are (fp32 ones not).  opts: k_new and v_new must be NULL (TA_ERR_OPTS; tree_attn_q8_append
  * writes the tree tokens); kernel TA_KERNEL_GENERIC names the scalar kernel, TA_KERNEL_MFMA (or _BASIC) the matrix-core one, which
- * takes head_dim 64 or 128, power-of-two pages or contiguous, 16-byte aligned q, K and V rows, and at most 256 query heads per
- * KV head.
+ * takes head_dim 64 or 128, pages of a power of two of at least 16 tokens or contiguous, 16-byte aligned q, K and V rows, cache
+ * strides below 2^31, and at most 256 query heads per KV head.
  * A NaN among the codes or scales that a row attends to makes it NaN; one that it does not attend to changes nothing.
  */
 int tree_attn_q8_fwd(const ta_tensor *q, const ta_tensor *k_cache, const ta_tensor *v_cache, const ta_tensor *k_scale,

@@ -222,14 +222,16 @@ int plan_mfma(const ta_tensor *out, const ta_opts *opts, int num_cus, TAProblem 
     // (256 rows, 4 requests of 131072 tokens: 856, 712 and 617 us, and 961 in blocks of 32; 64 rows, 32 requests of 8192 tokens: 90, 113
     // and 168 us, and 101).
     const int sizes[3] = {64, 128, 256}, costs[3] = {107, 178, 308};
-    p.ks_rows = 32;
-    for (int64_t i = 0, least = INT64_MAX; p.rows > 32 && i < 3; ++i) {
+    p.ks_rows = p.is_bf16 ? 32 : 128;
+    for (int64_t i = 0, least = INT64_MAX; p.is_bf16 && p.rows > 32 && i < 3; ++i) {
         const int64_t cost = (int64_t)((p.rows + sizes[i] - 1) / sizes[i]) * costs[i];
         if (cost < least) {
             least = cost;
             p.ks_rows = sizes[i];
         }
     }
+    // (fp32 queries, each the sum of three bf16 numbers, have blocks of 128 rows: 128 requests with 8 rows and 8192 tokens 168 us, and
+    // 1674 with the scalar kernel; 32 requests with 64 rows, 8 KV heads, 4096 tokens 177 and 6560)
     pl.ks_rows = p.ks_rows;
     p.basic = p.ks_rows == 32;
     const int blocks = (p.rows + p.ks_rows - 1) / p.ks_rows;
@@ -252,8 +254,8 @@ int plan_mfma(const ta_tensor *out, const ta_opts *opts, int num_cus, TAProblem 
     const bool out_aligned = ((uintptr_t)out->data % 16) == 0 && p.o_sb % 4 == 0 && p.o_st % 4 == 0 && p.o_sh % 4 == 0;
     const int64_t parts = (pl.n_wg + l1 - 1) / l1 + 1;
     p.merge_kind = !out_aligned ? TA_MERGE_GENERAL : parts >= 13 && lists * p.rows <= 1024 ? TA_MERGE_WIDE : TA_MERGE_ROW;
-    p.part_q15 = 1;
-    p.ls = 2;
+    p.part_q15 = p.is_bf16;                                // (fp32 queries keep fp32 partial results)
+    p.ls = p.is_bf16 ? 2 : 1;
     p.one_parts = 0;
     if (lists == 1 && num_splits == 0 && p.merge_kind == TA_MERGE_WIDE && pl.n_wg > 8192 / p.D)
         p.one_parts = 8192 / p.D;
@@ -263,10 +265,24 @@ int plan_mfma(const ta_tensor *out, const ta_opts *opts, int num_cus, TAProblem 
     const size_t rows_total = (size_t)pl.n_slots * p.rows_grp;
     pr->ws_o_bytes = ta_host_align_up(rows_total * p.D * sizeof(float), 256);
     pr->ws_lse_bytes = ta_host_align_up(rows_total * sizeof(float), 256);
-    pr->ws_ls_off = ta_host_align_up(rows_total * p.D * 2, 256);
+    pr->ws_ls_off = p.part_q15 ? ta_host_align_up(rows_total * p.D * 2, 256) : pr->ws_o_bytes;
     pr->ws_bytes = pr->ws_o_bytes + pr->ws_lse_bytes + ta_host_align_up((size_t)lists * 2 * sizeof(int32_t), 256);
-    if (num_splits == 0 && item_cost == 0 && lists > 0 && p.merge_kind != TA_MERGE_GENERAL && tiles_cap / lists <= 18)
-        p.solo = lists * blocks <= num_cus ? TA_SOLO_WIDE : p.basic ? TA_SOLO_PAIR : 0;
+    // Short lists go to one workgroup each, which writes the outputs itself: no schedule, no partial results, no merge pass.  Up to
+    // how many tiles depends on what a tile takes the workgroup, and on how many stand idle meanwhile (us per call, uncut / cut):
+    //     rows        8 lists                     64 lists                    256 lists
+    //     32          24 tiles 12.0/13.0          32 tiles 14.0/16.9          32 tiles 16.6/22.0
+    //                 48       16.0/13.3          64       20.3/16.7          64       26.3/31.9
+    //     64           8       14.0/15.9          16       18.3/19.3          32       27.2/30.9
+    //                 16       17.8/16.1          24       21.8/19.5          64       42.1/43.0
+    //     256          4       21.8/26.5           8       27.1/29.8          32       60.3/72.9
+    //                  8       26.5/25.4          24       44.5/33.2          64       96.7/105.6
+    //     fp32         4       13.3/17.2           8       19.0/21.6          24       40.7/42.4
+    //                  8       18.6/18.2          16       28.9/24.4          48       71.8/69.9
+    // (A batch of uneven lengths waits for its longest list: the line for a full chip stays where the gain is a fifth.)
+    const int64_t groups = lists * blocks;
+    const int line = 4 * groups >= 3 * num_cus ? 32 : p.basic ? 30 : p.ks_rows == 64 ? 14 : 7;
+    if (num_splits == 0 && item_cost == 0 && lists > 0 && p.merge_kind != TA_MERGE_GENERAL && tiles_cap / lists <= line)
+        p.solo = groups <= num_cus ? TA_SOLO_WIDE : p.basic ? TA_SOLO_PAIR : 0;
     if (p.solo)
         pl.merge_wgs = 0;
     return TA_OK;
@@ -498,7 +514,7 @@ int ta_host_build_q8_problem(const ta_tensor *q, const ta_tensor *k, const ta_te
         return TA_ERR_SHAPE;
     pr.plan.table_row = -1;
     auto in_32_bits = [](const ta_tensor *t) { return t->stride[0] < INT32_MAX && t->stride[2] < INT32_MAX; };
-    const bool mfma_ok = q->dtype == TA_BF16 && (pr.p.D == 64 || pr.p.D == 128) && (!pt || pr.p.ps_shift >= 4) && pr.p.G <= 256 &&
+    const bool mfma_ok = (pr.p.D == 64 || pr.p.D == 128) && (!pt || pr.p.ps_shift >= 4) && pr.p.G <= 256 &&
                          on_16_bytes(q) && on_16_bytes(k) && on_16_bytes(v) && in_32_bits(k) && in_32_bits(v) && in_32_bits(ks) &&
                          in_32_bits(vs);
     if (!mfma_ok && (kernel == TA_KERNEL_MFMA || kernel == TA_KERNEL_MFMA_BASIC))
@@ -582,6 +598,8 @@ int tree_attn_q8_plan(const ta_tensor *q, const ta_tensor *k_cache, const ta_ten
     if (rc != TA_OK)
         return rc;
     ta_host_fill_plan(qp.pr, plan);
+    if (qp.pr.plan.kernel == TA_KERNEL_MFMA)
+        plan[15] = qp.pr.plan.ks_rows;
     return TA_OK;
 }
 

@@ -1,4 +1,4 @@
-// KV pass over the 8-bit cache for many query rows (gfx950): bf16 queries, head_dim 64 or 128, fp32 accumulation.
+// KV pass over the 8-bit cache for many query rows, and for fp32 queries (gfx950): head_dim 64 or 128, fp32 accumulation.
 //
 // A workgroup of eight waves keeps 32 RBW rows (64, 128 or 256) of one (request, KV head) and walks its share in tiles of 128 tokens.
 // The codes of a tile become bf16 values once per workgroup: every wave loads sixteen tokens' codes and scales into registers two
@@ -11,6 +11,10 @@
 // Where every wave converts for itself (ta_q8_attn.hip) a run of 32 tokens costs it 64 conversions beside 16 products of 32 cycles,
 // and the loads' addresses on top.  The tokens of the tree follow the prefix without a gap, in the same tiles; a row's mask
 // is laid over the positions.
+//
+// An fp32 query is the sum of three bf16 numbers, exactly (8 bits of its 24 each), and so is a probability; K and V are bf16 as they
+// are, so three matrix products give what one in fp32 would.  Their first terms of Q stay in registers, the others in LDS, which
+// leaves room for tiles of 64 tokens at head_dim 128.  Not taken: the fp32 matrix instruction, a sixteenth of the bf16 one's rate.
 //
 // Two waves share a SIMD, w and w + 4, and one of them converts before its products, the other behind them (606 us without, at the
 // size below).  What bounds it is the matrix cores and the exponentials' unit in turn: 256 rows, 4 requests of 131072 tokens, 8 KV heads
@@ -27,7 +31,6 @@ typedef short qt_s4 __attribute__((ext_vector_type(4)));
 typedef short qt_s8 __attribute__((ext_vector_type(8)));
 typedef uint32_t qt_u32x4 __attribute__((ext_vector_type(4)));
 
-#define QT_TILE 128
 #define QT_LENS 256                              // batches of up to this many requests keep their lengths in LDS
 
 __device__ __forceinline__ float qt_swap_max(float x)      // over the two lanes that share a query row
@@ -51,37 +54,51 @@ __device__ __forceinline__ void qt_lds_barrier()           // (loads into regist
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
-template <int DH>
+template <int DH, bool F32>
 struct QtShape {
+    static constexpr int TOKENS = F32 && DH == 128 ? 64 : 128;       // of a tile
     static constexpr int ROW = 2 * DH;                     // bytes of a token row in LDS
-    static constexpr int TILE = QT_TILE * ROW;             // of a tile's K (or V)
+    static constexpr int TILE = TOKENS * ROW;             // of a tile's K (or V)
     static constexpr int BUF = 2 * TILE;
     static constexpr int LPR = DH / 16;                    // lanes of a row as it is loaded
     static constexpr int RPL = 64 / LPR;                   // rows of a load
-    static constexpr int NL = 16 / RPL;                    // loads of a wave's sixteen rows of K (or V)
+    static constexpr int TPW = TOKENS / 8;                 // tokens that a wave loads
+    static constexpr int NL = TPW / RPL;                   // loads of those of K (or V)
     static constexpr int STAGE = 32 * DH * 4;              // a wave's results at the end
-    static constexpr int FIXED = 2 * BUF + 4 * 8 * 2 * 32 + 4 * 8 + 8 + 8;
-    static_assert(8 * STAGE <= 2 * BUF, "results are staged in the tiles' place");
+    static constexpr int QL = F32 ? 2 * 128 * ROW : 0;     // second and third terms of the queries
+    static constexpr int TILES = 2 * BUF + QL;
+    static constexpr int FIXED = TILES + 4 * 8 * 2 * 32 + 4 * 8 + 8 + 8;
+    static_assert(8 * STAGE <= TILES, "results are staged in the tiles' place");
 };
 
 enum { QT_CUT, QT_SOLO };                                  // see ta_q8_attn.hip
 
-template <int DH, int MODE>
+template <int DH, bool F32, int MODE>
 static constexpr size_t qt_smem(int B)
 {
-    return QtShape<DH>::FIXED + (MODE == QT_SOLO || B <= TA_WAVE ? 0 : sizeof(int) * (B + 2 + (B <= QT_LENS ? 2 * B : 0)));
+    return QtShape<DH, F32>::FIXED + (MODE == QT_SOLO || B <= TA_WAVE ? 0 : sizeof(int) * (B + 2 + (B <= QT_LENS ? 2 * B : 0)));
 }
 
-template <int DH, int RBW, int MODE>
+// Two numbers' upper halves: their leading eight bits as bf16, exact, and what the numbers lose by it.
+__device__ __forceinline__ uint32_t qt_split(float &x, float &y)
+{
+    const uint32_t a = __float_as_uint(x), b = __float_as_uint(y);
+    x -= __uint_as_float(a & 0xffff0000u);
+    y -= __uint_as_float(b & 0xffff0000u);
+    return __builtin_amdgcn_perm(b, a, 0x07060302u);
+}
+
+template <int DH, int RBW, int MODE, bool F32>
 __global__ __launch_bounds__(512, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS, TAQ8Params p)
 {
     const TASched sc = TA_SCHED;
-    using C = QtShape<DH>;
+    using C = QtShape<DH, F32>;
     constexpr bool SOLO = MODE == QT_SOLO;
-    constexpr int KW = 8 / RBW, NR = 4 / KW;                             // waves that share rows, runs of a tile for each of them
+    constexpr int KW = 8 / RBW, NR = C::TOKENS / 32 / KW;                             // waves that share rows, runs of a tile for each of them
+    constexpr int TERMS = F32 ? 3 : 1;                                   // bf16 numbers whose sum is a query's or a probability's
     constexpr int NKK = DH / 16, NDB = DH / 32, NL = C::NL, ROWS = 32 * RBW;
     extern __shared__ __attribute__((aligned(16))) char smem[];
-    float *const stat = (float *)(smem + 2 * C::BUF);                    // [8][2][32]: reference and sum
+    float *const stat = (float *)(smem + C::TILES);                      // [8][2][32]: reference and sum
     int *const wbad = (int *)(stat + 8 * 2 * 32);                        // [8]: TA_STATUS_* bits a wave has met
     unsigned long long *const nan_nodes = (unsigned long long *)(wbad + 8);   // nodes whose values hold a NaN
     int *const cum = (int *)(nan_nodes + 2);                             // more than 64 requests: [B + 1] schedule
@@ -194,7 +211,7 @@ __global__ __launch_bounds__(512, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS, TAQ
             first = has_tree && j0 == n_b - 1 ? L : max((tile0 + j0) * TA_TILE, S);
             end = has_tree ? L + sc.T : min((tile0 + j1) * TA_TILE, L);
             base = first & ~31;
-            n_t = !ok ? 0 : (end - base + QT_TILE - 1) / QT_TILE;
+            n_t = !ok ? 0 : (end - base + C::TOKENS - 1) / C::TOKENS;
             return true;
         }
         return false;
@@ -209,7 +226,7 @@ __global__ __launch_bounds__(512, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS, TAQ
         // ---- what the start of an item needs: Q, the tree, page ids of this wave's tokens (lane l: tile pg_base + l)
         int pg = 0, pg_base = 0;
         auto load_pages = [&](int from) {
-            const int pos = base + (from + lane) * QT_TILE + 16 * wave;
+            const int pos = base + (from + lane) * C::TOKENS + C::TPW * wave;
             const int at = min(max(pos, first), end - 1);
             return p.page_table[(int64_t)b * p.pt_sb + (at >> p.ps_shift)];
         };
@@ -224,14 +241,29 @@ __global__ __launch_bounds__(512, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS, TAQ
         if (!bad && paged)
             pg = load_pages(0);
         uint4 qf[NKK];
+        uint4 *const ql = (uint4 *)(smem + 2 * C::BUF) + rb * NKK * TA_WAVE + lane;
         {
             // rows past the group's end repeat its first row (their results are never stored)
             const int row = rb * 32 + r32, R = row0 + (row < rows_here ? row : 0);
             const int node = (int)__umulhi((uint32_t)R << 8, p.g_magic);              // R / G
-            const uint16_t *q = (const uint16_t *)p.q + (int64_t)b * p.q_sb + (int64_t)node * p.q_st + (int64_t)(g * p.G + R - node * p.G) * p.q_sh;
+            const int64_t at = (int64_t)b * p.q_sb + (int64_t)node * p.q_st + (int64_t)(g * p.G + R - node * p.G) * p.q_sh + 8 * hf;
 #pragma unroll
-            for (int kk = 0; kk < NKK; ++kk)
-                qf[kk] = *(const uint4 *)(q + 16 * kk + 8 * hf);
+            for (int kk = 0; kk < NKK; ++kk) {
+                if constexpr (F32) {
+                    const float4 x0 = *(const float4 *)((const float *)p.q + at + 16 * kk), x1 = *(const float4 *)((const float *)p.q + at + 16 * kk + 4);
+                    float x[8] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
+#pragma unroll
+                    for (int t = 0; t < TERMS; ++t) {
+                        const uint4 y = make_uint4(qt_split(x[0], x[1]), qt_split(x[2], x[3]), qt_split(x[4], x[5]), qt_split(x[6], x[7]));
+                        if (t == 0)
+                            qf[kk] = y;
+                        else if (kg == 0)                              // (the waves that share rows share these)
+                            ql[((t - 1) * RBW * NKK + kk) * TA_WAVE] = y;
+                    }
+                } else {
+                    qf[kk] = *(const uint4 *)((const uint16_t *)p.q + at + 16 * kk);
+                }
+            }
         }
         int parent = 0;
         unsigned long long gmask = 0;
@@ -254,7 +286,7 @@ __global__ __launch_bounds__(512, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS, TAQ
                 pg_base = j;                                           // (waits)
                 pg = checked(load_pages(pg_base));
             }
-            const int pos0 = base + j * QT_TILE + 16 * wave;
+            const int pos0 = base + j * C::TOKENS + C::TPW * wave;
             const uint32_t page = (uint32_t)__builtin_amdgcn_readlane(paged ? pg : b, paged ? j - pg_base : 0);
             const uint32_t sl0 = (uint32_t)(paged ? pos0 & (p.ps - 1) : pos0);
             // (bases are scalars, and the lanes' offsets fit in 32 bits: the host has seen to it)
@@ -277,11 +309,11 @@ __global__ __launch_bounds__(512, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS, TAQ
             if (j >= n_t)
                 return;
             char *const kt = smem + (j & 1) * C::BUF, *const vt = kt + C::TILE;
-            const int pos0 = base + j * QT_TILE + 16 * wave;
-            const bool edge = pos0 < first || pos0 + 16 > min(L, end);
+            const int pos0 = base + j * C::TOKENS + C::TPW * wave;
+            const bool edge = pos0 < first || pos0 + C::TPW > min(L, end);
 #pragma unroll
             for (int i = 0; i < NL; ++i) {
-                const int row = 16 * wave + i * C::RPL + lrow;
+                const int row = C::TPW * wave + i * C::RPL + lrow;
                 qt_u32x4 k = x.k[i], v = x.v[i];
                 uint32_t ks = x.ks[i], vs = x.vs[i];
                 if (edge) {
@@ -368,7 +400,11 @@ __global__ __launch_bounds__(512, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS, TAQ
 #pragma unroll
             for (int kk = 0; kk < NKK; ++kk) {
                 const uint4 kf = *(const uint4 *)(smem + (ka ^ (kk << 5)));
-                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(qt_bf16x8, kf), __builtin_bit_cast(qt_bf16x8, qf[kk]), s, 0, 0, 0);
+#pragma unroll
+                for (int t = TERMS - 1; t >= 0; --t) {
+                    const uint4 qk = t == 0 ? qf[kk] : ql[((t - 1) * RBW * NKK + kk) * TA_WAVE];
+                    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(qt_bf16x8, kf), __builtin_bit_cast(qt_bf16x8, qk), s, 0, 0, 0);
+                }
             }
             // ---- V fragments: the first half is requested here and arrives under the softmax, the second under the products of the first
             typedef __attribute__((address_space(3))) qt_s4 *lds_s4;
@@ -425,24 +461,33 @@ __global__ __launch_bounds__(512, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS, TAQ
                         o[db][i] *= alpha;
             }
             const float neg_m = m_run == -INFINITY ? 0.f : -m_run;
-            uint32_t pk[8];
+            uint32_t pk[TERMS][8];
             float sum[2] = {0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float e0 = __builtin_amdgcn_exp2f(fmaf(s[2 * i], c, neg_m)), e1 = __builtin_amdgcn_exp2f(fmaf(s[2 * i + 1], c, neg_m));
+                float e0 = __builtin_amdgcn_exp2f(fmaf(s[2 * i], c, neg_m)), e1 = __builtin_amdgcn_exp2f(fmaf(s[2 * i + 1], c, neg_m));
                 sum[i & 1] += e0 + e1;
-                pk[i] = q8_pack_bf16(e0, e1);
+                if constexpr (F32) {
+#pragma unroll
+                    for (int t = 0; t < TERMS; ++t)
+                        pk[t][i] = qt_split(e0, e1);
+                } else {
+                    pk[0][i] = q8_pack_bf16(e0, e1);
+                }
             }
             l_run += sum[0] + sum[1];
             // ---- O^T += V^T . P^T
             __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) {
-                const uint4 pb = make_uint4(pk[4 * kb], pk[4 * kb + 1], pk[4 * kb + 2], pk[4 * kb + 3]);
 #pragma unroll
                 for (int db = 0; db < NDB; ++db) {
-                    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(qt_bf16x8, vf[db]), __builtin_bit_cast(qt_bf16x8, pb),
-                                                                    o[db], 0, 0, 0);
+#pragma unroll
+                    for (int t = TERMS - 1; t >= 0; --t) {
+                        const uint4 pb = make_uint4(pk[t][4 * kb], pk[t][4 * kb + 1], pk[t][4 * kb + 2], pk[t][4 * kb + 3]);
+                        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(qt_bf16x8, vf[db]), __builtin_bit_cast(qt_bf16x8, pb),
+                                                                        o[db], 0, 0, 0);
+                    }
                     if (kb == 0)
                         vf[db] = v_frag(1, db);
                 }
@@ -457,7 +502,7 @@ __global__ __launch_bounds__(512, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS, TAQ
             const int tile = (j & 1) * C::BUF;
 #pragma unroll 1
             for (int r = 0; r < NR; ++r) {
-                const int at = 32 * (kg + KW * r), pos0 = base + j * QT_TILE + at;
+                const int at = 32 * (kg + KW * r), pos0 = base + j * C::TOKENS + at;
                 if (pos0 < end && pos0 + 32 > first)
                     run(tile, at, pos0);
             }
@@ -555,14 +600,31 @@ __global__ __launch_bounds__(512, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS, TAQ
                     // (no merge: the rules are those of ta_q8_attn.hip)
                     const int R = row0 + row, node = (int)__umulhi((uint32_t)R << 8, p.g_magic), h = g * p.G + R - node * p.G;
                     const bool nan = any_bad || nan_seen || amax == INFINITY || lse2 != lse2;
-                    uint32_t *dst = (uint32_t *)((uint16_t *)p.out + (int64_t)b * p.o_sb + (int64_t)node * p.o_st + (int64_t)h * p.o_sh + 4 * c0);
+                    const int64_t at = (int64_t)b * p.o_sb + (int64_t)node * p.o_st + (int64_t)h * p.o_sh + 4 * c0;
+                    if constexpr (F32) {
+                        const float qnan = __uint_as_float(0x7fc00000u);
 #pragma unroll
-                    for (int q = 0; q < CPT / 4; ++q)
-                        *(uint2 *)(dst + 2 * q) = nan ? make_uint2(0x7fc07fc0u, 0x7fc07fc0u)
-                                                      : make_uint2(q8_pack_bf16(acc[4 * q], acc[4 * q + 1]), q8_pack_bf16(acc[4 * q + 2], acc[4 * q + 3]));
+                        for (int q = 0; q < CPT / 4; ++q)
+                            *(float4 *)((float *)p.out + at + 4 * q) = any_bad || lse2 != lse2 ? make_float4(qnan, qnan, qnan, qnan)
+                                : make_float4(acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]);
+                    } else {
+                        uint32_t *dst = (uint32_t *)((uint16_t *)p.out + at);
+#pragma unroll
+                        for (int q = 0; q < CPT / 4; ++q)
+                            *(uint2 *)(dst + 2 * q) = nan ? make_uint2(0x7fc07fc0u, 0x7fc07fc0u)
+                                : make_uint2(q8_pack_bf16(acc[4 * q], acc[4 * q + 1]), q8_pack_bf16(acc[4 * q + 2], acc[4 * q + 3]));
+                    }
                     if (p.lse && tid % 16 == 0)
                         p.lse[(int64_t)b * p.lse_sb + (int64_t)h * p.lse_sh + (int64_t)node * p.lse_st] =
                             lse2 == -INFINITY ? __uint_as_float(0x7fc00000u) : lse2 * 0.6931471805599453f;
+                } else if constexpr (F32) {
+                    const int64_t wrow = ta_ws_row(p, slot, 0, row0 + row);
+                    float *dst = (float *)ta_part_row(p, wrow) + 4 * c0;
+#pragma unroll
+                    for (int q = 0; q < CPT / 4; ++q)
+                        *(float4 *)(dst + 4 * q) = make_float4(acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]);
+                    if (tid % 16 == 0)
+                        p.ws_lse[wrow] = lse2;
                 } else {
                     float scale, to_q;
                     ta_q15_scale(amax, nan_seen, scale, to_q);
@@ -584,20 +646,20 @@ __global__ __launch_bounds__(512, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS, TAQ
     }
 }
 
-template <int DH, int RBW, int MODE>
+template <int DH, int RBW, int MODE, bool F32>
 static hipError_t launch_tile(const TAQ8Params &p, hipStream_t stream, int dev)
 {
-    const size_t smem = qt_smem<DH, MODE>(p.B);
-    static_assert(qt_smem<DH, MODE>(TA_MAX_BATCH) <= 160 * 1024, "whatever the batch");
+    const size_t smem = qt_smem<DH, F32, MODE>(p.B);
+    static_assert(qt_smem<DH, F32, MODE>(TA_MAX_BATCH) <= 160 * 1024, "whatever the batch");
     static bool attr_set[64] = {};      // per device and instance; setting it twice is harmless
     if (!attr_set[dev]) {
-        hipError_t e = hipFuncSetAttribute((const void *)ta_q8_tile_kernel<DH, RBW, MODE>, hipFuncAttributeMaxDynamicSharedMemorySize,
+        hipError_t e = hipFuncSetAttribute((const void *)ta_q8_tile_kernel<DH, RBW, MODE, F32>, hipFuncAttributeMaxDynamicSharedMemorySize,
                                            160 * 1024);
         if (e != hipSuccess)
             return e;
         attr_set[dev] = true;
     }
-    hipLaunchKernelGGL((ta_q8_tile_kernel<DH, RBW, MODE>), dim3(MODE == QT_SOLO ? p.B * p.Hkv : p.n_wg, (p.rows + 32 * RBW - 1) / (32 * RBW)),
+    hipLaunchKernelGGL((ta_q8_tile_kernel<DH, RBW, MODE, F32>), dim3(MODE == QT_SOLO ? p.B * p.Hkv : p.n_wg, (p.rows + 32 * RBW - 1) / (32 * RBW)),
                        dim3(512), smem, stream, TA_SCHED_ARGS(p), p);
     return hipGetLastError();
 }
@@ -606,17 +668,21 @@ hipError_t ta_launch_q8_tile(const TAQ8Params &p, hipStream_t stream, int dev)
 {
     if (dev < 0 || dev >= 64)
         return hipErrorInvalidDevice;
-    if (!p.part_q15 || p.ls != 2 || !p.is_bf16 || p.direct || (!p.solo && p.rows_grp % p.ks_rows != 0))
+    if (p.direct || (!p.solo && p.rows_grp % p.ks_rows != 0) || p.part_q15 != p.is_bf16 || p.ls != (p.is_bf16 ? 2 : 1) ||
+        (!p.is_bf16 && p.ks_rows != 128))
         return hipErrorInvalidValue;
-    auto with = [&](auto dh, auto rbw) {
+    auto with = [&](auto dh, auto rbw, auto f32) {
         constexpr int D = decltype(dh)::value, W = decltype(rbw)::value;
-        return p.solo ? launch_tile<D, W, QT_SOLO>(p, stream, dev) : launch_tile<D, W, QT_CUT>(p, stream, dev);
+        constexpr bool F32 = decltype(f32)::value;
+        return p.solo ? launch_tile<D, W, QT_SOLO, F32>(p, stream, dev) : launch_tile<D, W, QT_CUT, F32>(p, stream, dev);
     };
     auto rows = [&](auto dh) {
+        if (!p.is_bf16)
+            return with(dh, std::integral_constant<int, 4>{}, std::true_type{});
         switch (p.ks_rows) {
-        case 64: return with(dh, std::integral_constant<int, 2>{});
-        case 128: return with(dh, std::integral_constant<int, 4>{});
-        case 256: return with(dh, std::integral_constant<int, 8>{});
+        case 64: return with(dh, std::integral_constant<int, 2>{}, std::false_type{});
+        case 128: return with(dh, std::integral_constant<int, 4>{}, std::false_type{});
+        case 256: return with(dh, std::integral_constant<int, 8>{}, std::false_type{});
         default: return hipErrorInvalidValue;
         }
     };

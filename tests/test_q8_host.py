@@ -159,6 +159,29 @@ def test_plan_of_the_scalar_kernel():
     assert _plan(_good(), kernel=ta.TA_KERNEL_GENERIC)["kernel"] == ta.TA_KERNEL_GENERIC
 
 
+def test_plan_of_the_matrix_core_kernels():
+    """Who takes a call, in what blocks of rows, and whether lists are cut."""
+    def plan(**kw):
+        return _plan(_good(**{k: v for k, v in kw.items() if k not in ("num_splits", "kernel")}),
+                     **{k: v for k, v in kw.items() if k in ("num_splits", "kernel")})
+
+    for dt in (BF, F32):
+        for D in (64, 128):
+            assert plan(D=D, dt=dt)["kernel"] == ta.TA_KERNEL_MFMA
+            assert plan(D=D, dt=dt, kernel=ta.TA_KERNEL_MFMA)["kernel"] == ta.TA_KERNEL_MFMA
+        for kw in (dict(ps=8), dict(ps=48), dict(D=96), dict(D=32)):
+            assert plan(dt=dt, **kw)["kernel"] == ta.TA_KERNEL_GENERIC
+            with pytest.raises(ta.TreeAttnError):
+                plan(dt=dt, kernel=ta.TA_KERNEL_MFMA, **kw)
+    # two groups of four heads: T 8 has 32 rows, 9 has 36, 64 has 256
+    rows = {T: plan(T=T)["workgroup_rows"] for T in (1, 8, 9, 16, 17, 32, 33, 64)}
+    assert rows == {1: 32, 8: 32, 9: 64, 16: 64, 17: 128, 32: 128, 33: 256, 64: 256}
+    assert plan(T=1, dt=F32)["workgroup_rows"] == plan(T=64, dt=F32)["workgroup_rows"] == 128
+    # short lists are not cut and need no merge, unless the caller says how
+    assert plan(max_pages=4)["merge_workgroups"] == 0 and plan(max_pages=200)["merge_workgroups"] > 0
+    assert plan(max_pages=4, num_splits=2)["merge_workgroups"] > 0
+
+
 def test_random_descriptors_never_break_the_host_code():
     """Random ranks, shapes and strides through the checks of every call: any status is fine, as long as it is one."""
     rng = np.random.default_rng(7)
