@@ -216,7 +216,6 @@ int plan_mfma(const ta_tensor *out, const ta_opts *opts, int num_cus, TAProblem 
     const int64_t lists = (int64_t)p.B * p.Hkv, l1 = lists > 0 ? lists : 1;
     const int64_t tiles_cap = lists * ((p.capacity - p.T + TA_TILE - 1) / TA_TILE + 1);
     pl.kernel = TA_KERNEL_MFMA;
-    pl.threads = 512;
     // Query rows of a workgroup.  Up to 32 have a kernel of their own (ta_q8_attn.hip: every wave for itself).  More of them
     // take tiles of 64, 128 or 256 rows, those that cost least: a pass over the keys takes 107, 178 and 308, relative to one another
     // (256 rows, 4 requests of 131072 tokens: 856, 712 and 617 us, and 961 in blocks of 32; 64 rows, 32 requests of 8192 tokens: 90, 113
@@ -242,7 +241,9 @@ int plan_mfma(const ta_tensor *out, const ta_opts *opts, int num_cus, TAProblem 
     if (tiles_cap + lists * p.pad > INT32_MAX)
         return TA_ERR_SHAPE;
     // workgroups side by side, one grid row apart, should fall on one XCD, where the keys come out of the L2 for all but the first
-    int64_t want = num_cus / blocks;
+    const bool pairs = p.is_bf16 && (p.ks_rows == 64 || p.ks_rows == 128);      // workgroups of four waves, two on a compute unit
+    pl.threads = pairs ? 256 : 512;
+    int64_t want = (pairs ? 2 : 1) * num_cus / blocks;
     if (blocks > 1 && want > 8)
         want -= want % 8;
     pl.n_wg = (int)(num_splits > 0 ? num_splits : want > 0 ? want : 1);
@@ -282,7 +283,7 @@ int plan_mfma(const ta_tensor *out, const ta_opts *opts, int num_cus, TAProblem 
     const int64_t groups = lists * blocks;
     const int line = 4 * groups >= 3 * num_cus ? 32 : p.basic ? 30 : p.ks_rows == 64 ? 14 : 7;
     if (num_splits == 0 && item_cost == 0 && lists > 0 && p.merge_kind != TA_MERGE_GENERAL && tiles_cap / lists <= line)
-        p.solo = groups <= num_cus ? TA_SOLO_WIDE : p.basic ? TA_SOLO_PAIR : 0;
+        p.solo = groups <= num_cus ? TA_SOLO_WIDE : p.basic || (pairs && groups <= 2 * num_cus) ? TA_SOLO_PAIR : 0;
     if (p.solo)
         pl.merge_wgs = 0;
     return TA_OK;
@@ -513,7 +514,7 @@ int ta_host_build_q8_problem(const ta_tensor *q, const ta_tensor *k, const ta_te
     if (pr.p.B > 0 && pr.p.n_pages < 1)
         return TA_ERR_SHAPE;
     pr.plan.table_row = -1;
-    auto in_32_bits = [](const ta_tensor *t) { return t->stride[0] < INT32_MAX && t->stride[2] < INT32_MAX; };
+    auto in_32_bits = [](const ta_tensor *t) { return t->stride[0] < INT32_MAX && t->stride[2] < INT32_MAX / 32; };    // (32 rows)
     const bool mfma_ok = (pr.p.D == 64 || pr.p.D == 128) && (!pt || pr.p.ps_shift >= 4) && pr.p.G <= 256 &&
                          on_16_bytes(q) && on_16_bytes(k) && on_16_bytes(v) && in_32_bits(k) && in_32_bits(v) && in_32_bits(ks) &&
                          in_32_bits(vs);

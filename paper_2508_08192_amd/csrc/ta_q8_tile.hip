@@ -54,29 +54,29 @@ __device__ __forceinline__ void qt_lds_barrier()           // (loads into regist
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
-template <int DH, bool F32>
+template <int DH, int NW, bool F32>
 struct QtShape {
-    static constexpr int TOKENS = F32 && DH == 128 ? 64 : 128;       // of a tile
+    static constexpr int TOKENS = F32 && DH == 128 ? 64 : 16 * NW;   // of a tile
     static constexpr int ROW = 2 * DH;                     // bytes of a token row in LDS
     static constexpr int TILE = TOKENS * ROW;             // of a tile's K (or V)
     static constexpr int BUF = 2 * TILE;
     static constexpr int LPR = DH / 16;                    // lanes of a row as it is loaded
     static constexpr int RPL = 64 / LPR;                   // rows of a load
-    static constexpr int TPW = TOKENS / 8;                 // tokens that a wave loads
+    static constexpr int TPW = TOKENS / NW;                // tokens that a wave loads
     static constexpr int NL = TPW / RPL;                   // loads of those of K (or V)
     static constexpr int STAGE = 32 * DH * 4;              // a wave's results at the end
     static constexpr int QL = F32 ? 2 * 128 * ROW : 0;     // second and third terms of the queries
     static constexpr int TILES = 2 * BUF + QL;
-    static constexpr int FIXED = TILES + 4 * 8 * 2 * 32 + 4 * 8 + 8 + 8;
-    static_assert(8 * STAGE <= TILES, "results are staged in the tiles' place");
+    static constexpr int FIXED = TILES + 4 * NW * 2 * 32 + 4 * 8 + 8 + 8;
+    static_assert(NW * STAGE <= TILES, "results are staged in the tiles' place");
 };
 
 enum { QT_CUT, QT_SOLO };                                  // see ta_q8_attn.hip
 
-template <int DH, bool F32, int MODE>
+template <int DH, int NW, bool F32, int MODE>
 static constexpr size_t qt_smem(int B)
 {
-    return QtShape<DH, F32>::FIXED + (MODE == QT_SOLO || B <= TA_WAVE ? 0 : sizeof(int) * (B + 2 + (B <= QT_LENS ? 2 * B : 0)));
+    return QtShape<DH, NW, F32>::FIXED + (MODE == QT_SOLO || B <= TA_WAVE ? 0 : sizeof(int) * (B + 2 + (B <= QT_LENS ? 2 * B : 0)));
 }
 
 // Two numbers' upper halves: their leading eight bits as bf16, exact, and what the numbers lose by it.
@@ -88,18 +88,18 @@ __device__ __forceinline__ uint32_t qt_split(float &x, float &y)
     return __builtin_amdgcn_perm(b, a, 0x07060302u);
 }
 
-template <int DH, int RBW, int MODE, bool F32>
-__global__ __launch_bounds__(512, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS, TAQ8Params p)
+template <int DH, int RBW, int NW, int MODE, bool F32>
+__global__ __launch_bounds__(64 * NW, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS, TAQ8Params p)
 {
     const TASched sc = TA_SCHED;
-    using C = QtShape<DH, F32>;
+    using C = QtShape<DH, NW, F32>;
     constexpr bool SOLO = MODE == QT_SOLO;
-    constexpr int KW = 8 / RBW, NR = C::TOKENS / 32 / KW;                             // waves that share rows, runs of a tile for each of them
+    constexpr int KW = NW / RBW, NR = C::TOKENS / 32 / KW;                             // waves that share rows, runs of a tile for each of them
     constexpr int TERMS = F32 ? 3 : 1;                                   // bf16 numbers whose sum is a query's or a probability's
     constexpr int NKK = DH / 16, NDB = DH / 32, NL = C::NL, ROWS = 32 * RBW;
     extern __shared__ __attribute__((aligned(16))) char smem[];
-    float *const stat = (float *)(smem + C::TILES);                      // [8][2][32]: reference and sum
-    int *const wbad = (int *)(stat + 8 * 2 * 32);                        // [8]: TA_STATUS_* bits a wave has met
+    float *const stat = (float *)(smem + C::TILES);                      // [NW][2][32]: reference and sum
+    int *const wbad = (int *)(stat + NW * 2 * 32);                       // [NW]: TA_STATUS_* bits a wave has met
     unsigned long long *const nan_nodes = (unsigned long long *)(wbad + 8);   // nodes whose values hold a NaN
     int *const cum = (int *)(nan_nodes + 2);                             // more than 64 requests: [B + 1] schedule
     int *const lens = cum + sc.B + 1, *const starts = lens + sc.B;       // and, up to QT_LENS, lengths and window starts
@@ -147,7 +147,21 @@ __global__ __launch_bounds__(512, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS, TAQ
     const int vtk = 4 * hf + ((lane >> 2) & 3);
     const int vf_at = vtk * C::ROW + (lane & 3) * 8 + ((((lane >> 4) & 1) ^ vx(vtk)) << 5);
     const int lrow = lane / C::LPR, lchunk = lane % C::LPR;              // as a lane loads: its row of a load's, its sixteen columns
+    const bool s_is_v = lane % (2 * C::TPW) >= C::TPW;                   // of two lanes a token's scales
+    const uint32_t s_step = (uint32_t)(s_is_v ? p.vs_ss : p.ks_ss), s_lane = lane % C::TPW * s_step;
+    const uint32_t k_lane = lrow * (uint32_t)p.k_ss + 16u * lchunk, v_lane = lrow * (uint32_t)p.v_ss + 16u * lchunk;
+    int kw_at[NL][2], vw_at[NL][2];                                      // where their two halves go
+#pragma unroll
+    for (int i = 0; i < NL; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int row = C::TPW * wave + i * C::RPL + lrow;
+            kw_at[i][h] = row * C::ROW + (((2 * lchunk + h) ^ kx(row)) << 4);
+            vw_at[i][h] = row * C::ROW + (((2 * lchunk + h) ^ (2 * vx(row))) << 4);
+        }
 
+    typedef __attribute__((address_space(3))) char *lds_t;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_t)smem;              // (zero, but the compiler adds it to every address that it does not see)
     // ---- the current item: list (b, g), tokens at positions [first, end) of the request, those from L on being the tree's
     int b = -1, g = 0, slot = 0, L = 0, first = 0, end = 0, base = 0, n_t = 0, bad = 0;
     auto next_item = [&]() {
@@ -210,6 +224,10 @@ __global__ __launch_bounds__(512, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS, TAQ
             const bool has_tree = j1 == n_b;
             first = has_tree && j0 == n_b - 1 ? L : max((tile0 + j0) * TA_TILE, S);
             end = has_tree ? L + sc.T : min((tile0 + j1) * TA_TILE, L);
+            if (!ok) {                                                 // (its loads, which nobody uses, go to the first token of a page)
+                first = 0;
+                end = 1;
+            }
             base = first & ~31;
             n_t = !ok ? 0 : (end - base + C::TOKENS - 1) / C::TOKENS;
             return true;
@@ -219,7 +237,7 @@ __global__ __launch_bounds__(512, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS, TAQ
 
     struct Raw {                                           // a wave's sixteen tokens of a tile
         qt_u32x4 k[NL], v[NL];
-        uint32_t ks[NL], vs[NL];
+        uint32_t scale;                                    // lane l: K's of token l, V's of token l - TPW
     };
 
     while (next_item()) {
@@ -279,72 +297,90 @@ __global__ __launch_bounds__(512, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS, TAQ
         const uint8_t *const kgp = (const uint8_t *)p.k + (int64_t)g * p.k_sh, *const vgp = (const uint8_t *)p.v + (int64_t)g * p.v_sh;
         const uint8_t *const ksp = p.ks + (int64_t)g * p.ks_sh, *const vsp = p.vs + (int64_t)g * p.vs_sh;
 
+        // The loads of a tile, the same number whatever the tile, so that a wait can leave the next one's in flight: tokens outside
+        // [first, end) are read as the nearest that is in it, and the tiles behind the last as the last token.
         auto load_tile = [&](int j, Raw &x) {
-            if (j >= n_t)
-                return;
             if (paged && j - pg_base >= TA_WAVE) {
                 pg_base = j;                                           // (waits)
                 pg = checked(load_pages(pg_base));
             }
-            const int pos0 = base + j * C::TOKENS + C::TPW * wave;
+            const int pos0 = base + j * C::TOKENS + C::TPW * wave, at0 = min(max(pos0, first), end - 1) & -C::TPW;
             const uint32_t page = (uint32_t)__builtin_amdgcn_readlane(paged ? pg : b, paged ? j - pg_base : 0);
-            const uint32_t sl0 = (uint32_t)(paged ? pos0 & (p.ps - 1) : pos0);
+            const uint32_t sl0 = (uint32_t)(paged ? at0 & (p.ps - 1) : at0);
             // (bases are scalars, and the lanes' offsets fit in 32 bits: the host has seen to it)
             const uint8_t *kb = kgp + (uint64_t)page * (uint32_t)p.k_sp + (uint64_t)sl0 * (uint32_t)p.k_ss;
             const uint8_t *vb = vgp + (uint64_t)page * (uint32_t)p.v_sp + (uint64_t)sl0 * (uint32_t)p.v_ss;
-            const uint8_t *ksb = ksp + (uint64_t)page * (uint32_t)p.ks_sp + (uint64_t)sl0 * (uint32_t)p.ks_ss;
-            const uint8_t *vsb = vsp + (uint64_t)page * (uint32_t)p.vs_sp + (uint64_t)sl0 * (uint32_t)p.vs_ss;
-#pragma unroll
-            for (int i = 0; i < NL; ++i)
-                if (pos0 + i * C::RPL < end && pos0 + (i + 1) * C::RPL > first) {      // any token of these: their page is one of the request's
-                    // (rows past the last token are read as that one: a contiguous cache may end there)
-                    const uint32_t r = (uint32_t)(i * C::RPL + min(lrow, end - 1 - (pos0 + i * C::RPL)));
-                    x.k[i] = __builtin_nontemporal_load((const qt_u32x4 *)(kb + r * (uint32_t)p.k_ss + 16 * lchunk));
-                    x.v[i] = __builtin_nontemporal_load((const qt_u32x4 *)(vb + r * (uint32_t)p.v_ss + 16 * lchunk));
-                    x.ks[i] = ksb[r * (uint32_t)p.ks_ss];
-                    x.vs[i] = vsb[r * (uint32_t)p.vs_ss];
-                }
-        };
-        auto write_tile = [&](int j, Raw &x) {
-            if (j >= n_t)
-                return;
-            char *const kt = smem + (j & 1) * C::BUF, *const vt = kt + C::TILE;
-            const int pos0 = base + j * C::TOKENS + C::TPW * wave;
-            const bool edge = pos0 < first || pos0 + C::TPW > min(L, end);
+            const uint64_t ko = (uint64_t)page * (uint32_t)p.ks_sp + (uint64_t)sl0 * (uint32_t)p.ks_ss;
+            const uint64_t vo = (uint64_t)page * (uint32_t)p.vs_sp + (uint64_t)sl0 * (uint32_t)p.vs_ss;
+            uint32_t so = s_lane, koff[NL], voff[NL];
 #pragma unroll
             for (int i = 0; i < NL; ++i) {
-                const int row = C::TPW * wave + i * C::RPL + lrow;
-                qt_u32x4 k = x.k[i], v = x.v[i];
-                uint32_t ks = x.ks[i], vs = x.vs[i];
-                if (edge) {
+                koff[i] = k_lane + i * C::RPL * (uint32_t)p.k_ss;
+                voff[i] = v_lane + i * C::RPL * (uint32_t)p.v_ss;
+            }
+            if (pos0 < first || pos0 + C::TPW > end) {
+                const int hi = min(end - 1 - at0, C::TPW - 1), lo = pos0 >= end ? hi : max(first - at0, 0);
+                so = (uint32_t)min(max(lane % C::TPW, lo), hi) * s_step;
+#pragma unroll
+                for (int i = 0; i < NL; ++i) {
+                    const uint32_t r = (uint32_t)min(max(i * C::RPL + lrow, lo), hi);
+                    koff[i] = r * (uint32_t)p.k_ss + 16u * lchunk;
+                    voff[i] = r * (uint32_t)p.v_ss + 16u * lchunk;
+                }
+            }
+            x.scale = (s_is_v ? vsp + vo : ksp + ko)[so];
+#pragma unroll
+            for (int i = 0; i < NL; ++i) {
+                x.k[i] = __builtin_nontemporal_load((const qt_u32x4 *)(kb + koff[i]));
+                x.v[i] = __builtin_nontemporal_load((const qt_u32x4 *)(vb + voff[i]));
+            }
+        };
+        // into the tile at byte `buf` of LDS
+        auto write_tile = [&](int j, int buf, Raw &x) {
+            if (j >= n_t)
+                return;
+            const int pos0 = base + j * C::TOKENS + C::TPW * wave;
+            const bool edge = pos0 < first || pos0 + C::TPW > min(L, end);
+            const int scale = (int)__float_as_uint(q8_scale(x.scale));   // (one conversion per token and tensor, then sent to those who need it)
+            float kscale[NL], vscale[NL];
+#pragma unroll
+            for (int i = 0; i < NL; ++i) {
+                kscale[i] = __uint_as_float((uint32_t)__builtin_amdgcn_ds_bpermute(4 * lrow + 4 * i * C::RPL, scale));
+                vscale[i] = __uint_as_float((uint32_t)__builtin_amdgcn_ds_bpermute(4 * lrow + 4 * (C::TPW + i * C::RPL), scale));
+            }
+            if (edge) {
+#pragma unroll
+                for (int i = 0; i < NL; ++i) {
                     // tokens of others are zeros; a NaN among a node's values counts only for rows that attend to it, so it is noted
                     // and taken out of the product
                     const int pos = pos0 + i * C::RPL + lrow;
                     const bool mine = pos >= first && pos < end;
                     if (!mine) {
-                        k = qt_u32x4{0u, 0u, 0u, 0u};
-                        ks = 127u;
+                        x.k[i] = qt_u32x4{0u, 0u, 0u, 0u};
+                        kscale[i] = 1.f;
                     }
-                    uint32_t nan = vs == 255u ? 1u : 0u;
+                    uint32_t nan = vscale[i] != vscale[i] ? 1u : 0u;
 #pragma unroll
                     for (int n = 0; n < 4; ++n)
-                        nan |= ((v[n] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+                        nan |= ((x.v[i][n] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
                     if (mine && pos >= L && nan)
                         atomicOr(nan_nodes, 1ull << (pos - L));
                     if (!mine || (pos >= L && nan)) {
-                        v = qt_u32x4{0u, 0u, 0u, 0u};
-                        vs = 127u;
+                        x.v[i] = qt_u32x4{0u, 0u, 0u, 0u};
+                        vscale[i] = 1.f;
                     }
                 }
-                const float kscale = q8_scale(ks), vscale = q8_scale(vs);
+            }
+#pragma unroll
+            for (int i = 0; i < NL; ++i) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    *(uint4 *)(kt + row * C::ROW + (((2 * lchunk + h) ^ kx(row)) << 4)) =
-                        make_uint4(q8_bf16_2<false>(k[2 * h], kscale), q8_bf16_2<true>(k[2 * h], kscale),
-                                   q8_bf16_2<false>(k[2 * h + 1], kscale), q8_bf16_2<true>(k[2 * h + 1], kscale));
-                    *(uint4 *)(vt + row * C::ROW + (((2 * lchunk + h) ^ (2 * vx(row))) << 4)) =
-                        make_uint4(q8_bf16_2<false>(v[2 * h], vscale), q8_bf16_2<true>(v[2 * h], vscale),
-                                   q8_bf16_2<false>(v[2 * h + 1], vscale), q8_bf16_2<true>(v[2 * h + 1], vscale));
+                    typedef __attribute__((address_space(3))) qt_u32x4 *lds_u4;
+                    const uint32_t k0 = x.k[i][2 * h], k1 = x.k[i][2 * h + 1], v0 = x.v[i][2 * h], v1 = x.v[i][2 * h + 1];
+                    *(lds_u4)(uintptr_t)(lds0 + kw_at[i][h] + buf) =
+                        qt_u32x4{q8_bf16_2<false>(k0, kscale[i]), q8_bf16_2<true>(k0, kscale[i]), q8_bf16_2<false>(k1, kscale[i]), q8_bf16_2<true>(k1, kscale[i])};
+                    *(lds_u4)(uintptr_t)(lds0 + vw_at[i][h] + buf + C::TILE) =
+                        qt_u32x4{q8_bf16_2<false>(v0, vscale[i]), q8_bf16_2<true>(v0, vscale[i]), q8_bf16_2<false>(v1, vscale[i]), q8_bf16_2<true>(v1, vscale[i])};
                 }
             }
         };
@@ -386,7 +422,7 @@ __global__ __launch_bounds__(512, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS, TAQ
                 tmask = ((unsigned long long)m_hi << 32) | m_lo;
         }
         qt_lds_barrier();                                  // (nan_nodes is zero, and the tiles' place is free)
-        write_tile(0, even);
+        write_tile(0, 0, even);
         load_tile(2, even);
         qt_lds_barrier();
 
@@ -394,12 +430,12 @@ __global__ __launch_bounds__(512, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS, TAQ
         auto run = [&](int tile, int at, int pos0) {
             // ---- S^T = K . Q^T
             qt_f32x16 s = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            int ka = tile + at * C::ROW + kf_at, va = tile + C::TILE + at * C::ROW + vf_at;
+            uint32_t ka = lds0 + at * C::ROW + kf_at, va = lds0 + at * C::ROW + vf_at;
             asm volatile("" : "+v"(ka), "+v"(va));         // (one operation per address, where addresses that are kept would not fit in registers)
             __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int kk = 0; kk < NKK; ++kk) {
-                const uint4 kf = *(const uint4 *)(smem + (ka ^ (kk << 5)));
+                const qt_u32x4 kf = *(const __attribute__((address_space(3))) qt_u32x4 *)(uintptr_t)((ka ^ (kk << 5)) + tile);
 #pragma unroll
                 for (int t = TERMS - 1; t >= 0; --t) {
                     const uint4 qk = t == 0 ? qf[kk] : ql[((t - 1) * RBW * NKK + kk) * TA_WAVE];
@@ -409,9 +445,9 @@ __global__ __launch_bounds__(512, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS, TAQ
             // ---- V fragments: the first half is requested here and arrives under the softmax, the second under the products of the first
             typedef __attribute__((address_space(3))) qt_s4 *lds_s4;
             auto v_frag = [&](int kb, int db) {
-                const char *a = smem + (va ^ (db << 6)) + kb * 16 * C::ROW;
-                const qt_s4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)a);
-                const qt_s4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(a + 8 * C::ROW));
+                const uint32_t a = (va ^ (db << 6)) + tile + C::TILE + kb * 16 * C::ROW;
+                const qt_s4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(uintptr_t)a);
+                const qt_s4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(uintptr_t)(a + 8 * C::ROW));
                 return __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
             };
             qt_s8 vf[NDB];
@@ -440,15 +476,11 @@ __global__ __launch_bounds__(512, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS, TAQ
                         s[i] = -INFINITY;
             }
             // ---- running softmax (the reference moves only when a score exceeds it by more than 2^4: see ta_mfma_ks.hip)
-            float t0 = s[0], t1 = s[1], t2 = s[2], t3 = s[3];
+            float top = s[0];
 #pragma unroll
-            for (int i = 4; i < 16; i += 4) {
-                t0 = fmaxf(t0, s[i]);
-                t1 = fmaxf(t1, s[i + 1]);
-                t2 = fmaxf(t2, s[i + 2]);
-                t3 = fmaxf(t3, s[i + 3]);
-            }
-            const float top = fmaxf(fmaxf(t0, t1), fmaxf(t2, t3)) * c;
+            for (int i = 1; i < 16; ++i)
+                top = __builtin_elementwise_maximum(top, s[i]);          // (of a NaN a NaN, which moves nothing: such a row is NaN anyway)
+            top *= c;
             if (__any(top > m_run + (SOLO ? 0.f : 4.f))) {
                 const float m_new = fmaxf(m_run, qt_swap_max(top));
                 const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
@@ -494,29 +526,23 @@ __global__ __launch_bounds__(512, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS, TAQ
             }
             __builtin_amdgcn_s_setprio(0);
         };
-        auto step = [&](int j, Raw &next) {
-            if (wave < 4) {
-                write_tile(j + 1, next);
-                load_tile(j + 3, next);
-            }
-            const int tile = (j & 1) * C::BUF;
+        // (which of the two tiles in LDS is known where a step is compiled)
+        auto step = [&](int j, auto even_step, Raw &next) {
+            constexpr int BUF = decltype(even_step)::value ? 0 : C::BUF;
+            write_tile(j + 1, C::BUF - BUF, next);
+            load_tile(j + 3, next);
 #pragma unroll 1
             for (int r = 0; r < NR; ++r) {
                 const int at = 32 * (kg + KW * r), pos0 = base + j * C::TOKENS + at;
                 if (pos0 < end && pos0 + 32 > first)
-                    run(tile, at, pos0);
-            }
-            if (wave >= 4) {
-                write_tile(j + 1, next);
-                load_tile(j + 3, next);
+                    run(BUF, at, pos0);
             }
             qt_lds_barrier();
         };
 #pragma unroll 1
-        for (int j = 0; j < n_t; j += 2) {
-            step(j, odd);
-            if (j + 1 < n_t)
-                step(j + 1, even);
+        for (int j = 0; j < n_t; j += 2) {                 // (no way out in between: one more path here, and all waits are for everything)
+            step(j, std::true_type{}, odd);
+            step(j + 1, std::false_type{}, even);
         }
 
         // ---- results: each wave stages its 32 x DH block (16-byte chunk ch of row r at chunk ch ^ (r & 15)), then the threads add up
@@ -554,11 +580,11 @@ __global__ __launch_bounds__(512, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS, TAQ
         qt_lds_barrier();
         int any_bad = 0;
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
+        for (int k = 0; k < NW; ++k)
             any_bad |= wbad[k];
         constexpr int CPT = DH / 16;                       // columns of a thread: sixteen of them per row
 #pragma unroll 1
-        for (int row = tid / 16; row < ROWS; row += 32) {
+        for (int row = tid / 16; row < ROWS; row += 4 * NW) {
             const int c0 = (tid % 16) * (CPT / 4), rr = row & 31, wv0 = row / 32;
             float mw[KW], big = -INFINITY;
 #pragma unroll
@@ -646,21 +672,21 @@ __global__ __launch_bounds__(512, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS, TAQ
     }
 }
 
-template <int DH, int RBW, int MODE, bool F32>
+template <int DH, int RBW, int NW, int MODE, bool F32>
 static hipError_t launch_tile(const TAQ8Params &p, hipStream_t stream, int dev)
 {
-    const size_t smem = qt_smem<DH, F32, MODE>(p.B);
-    static_assert(qt_smem<DH, F32, MODE>(TA_MAX_BATCH) <= 160 * 1024, "whatever the batch");
+    const size_t smem = qt_smem<DH, NW, F32, MODE>(p.B);
+    static_assert(qt_smem<DH, NW, F32, MODE>(TA_MAX_BATCH) <= 160 * 1024, "whatever the batch");
     static bool attr_set[64] = {};      // per device and instance; setting it twice is harmless
     if (!attr_set[dev]) {
-        hipError_t e = hipFuncSetAttribute((const void *)ta_q8_tile_kernel<DH, RBW, MODE, F32>, hipFuncAttributeMaxDynamicSharedMemorySize,
+        hipError_t e = hipFuncSetAttribute((const void *)ta_q8_tile_kernel<DH, RBW, NW, MODE, F32>, hipFuncAttributeMaxDynamicSharedMemorySize,
                                            160 * 1024);
         if (e != hipSuccess)
             return e;
         attr_set[dev] = true;
     }
-    hipLaunchKernelGGL((ta_q8_tile_kernel<DH, RBW, MODE, F32>), dim3(MODE == QT_SOLO ? p.B * p.Hkv : p.n_wg, (p.rows + 32 * RBW - 1) / (32 * RBW)),
-                       dim3(512), smem, stream, TA_SCHED_ARGS(p), p);
+    hipLaunchKernelGGL((ta_q8_tile_kernel<DH, RBW, NW, MODE, F32>), dim3(MODE == QT_SOLO ? p.B * p.Hkv : p.n_wg, (p.rows + 32 * RBW - 1) / (32 * RBW)),
+                       dim3(64 * NW), smem, stream, TA_SCHED_ARGS(p), p);
     return hipGetLastError();
 }
 
@@ -674,7 +700,12 @@ hipError_t ta_launch_q8_tile(const TAQ8Params &p, hipStream_t stream, int dev)
     auto with = [&](auto dh, auto rbw, auto f32) {
         constexpr int D = decltype(dh)::value, W = decltype(rbw)::value;
         constexpr bool F32 = decltype(f32)::value;
-        return p.solo ? launch_tile<D, W, QT_SOLO, F32>(p, stream, dev) : launch_tile<D, W, QT_CUT, F32>(p, stream, dev);
+        if (p.solo == TA_SOLO_WIDE)
+            return launch_tile<D, W, 8, QT_SOLO, F32>(p, stream, dev);
+        constexpr int NW = W == 8 || F32 ? 8 : 4;
+        if (p.solo)
+            return NW == 4 ? launch_tile<D, W, NW, QT_SOLO, F32>(p, stream, dev) : hipErrorInvalidValue;
+        return launch_tile<D, W, NW, QT_CUT, F32>(p, stream, dev);
     };
     auto rows = [&](auto dh) {
         if (!p.is_bf16)
