@@ -94,6 +94,7 @@ struct TACompact {
 struct TAQ8Params : TAParams {
     const uint8_t *ks, *vs;            // [num_pages, Hkv, page_size]
     int64_t ks_sp, ks_sh, ks_ss, vs_sp, vs_sh, vs_ss;
+    int32_t waves;                     // of a workgroup of the tile kernel when lists are cut: 4 or 8
 };
 
 // A step's or a prompt's rows on their way: queries and keys to their positions (rotary embedding), keys and values into the

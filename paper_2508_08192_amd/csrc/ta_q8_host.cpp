@@ -236,12 +236,18 @@ int plan_mfma(const ta_tensor *out, const ta_opts *opts, int num_cus, TAProblem 
     const int blocks = (p.rows + p.ks_rows - 1) / p.ks_rows;
     p.rows_grp = pl.rows_grp = blocks * p.ks_rows;
     p.n_rg = pl.n_rg = 1;
-    pl.item_cost = item_cost > 0 ? item_cost : lists == 1 ? 6 : 9;
+    // (what a share of a list costs beside its tiles: 128 requests of 8 KV heads, one new token, 15 105 us, 9 117; 20 costs 1 % more.
+    // With tiles for all waves 9 to 13 are the same within 2 %.)
+    pl.item_cost = item_cost > 0 ? item_cost : lists == 1 ? 6 : p.basic ? 15 : 9;
     p.pad = pl.item_cost - 1;
     if (tiles_cap + lists * p.pad > INT32_MAX)
         return TA_ERR_SHAPE;
     // workgroups side by side, one grid row apart, should fall on one XCD, where the keys come out of the L2 for all but the first
-    const bool pairs = p.is_bf16 && (p.ks_rows == 64 || p.ks_rows == 128);      // workgroups of four waves, two on a compute unit
+    // Workgroups of four waves, two on a compute unit, wait for one another less, and take more shares, each with its start and its
+    // partial results: 64 rows, 64 requests of 8 KV heads, 512 to 4096 tokens 52 us, 60 with eight waves; 32 of 512 to 8192: 84 and
+    // 88; but 8 of 4096: 31 and 29, and 128 rows in one request of 8192: 34 and 31.  (Up to 32 rows: 128 requests, one new token 112 us,
+    // 105 with eight waves.)
+    const bool small_blocks = p.is_bf16 && (p.ks_rows == 64 || p.ks_rows == 128), pairs = small_blocks && tiles_cap >= 64 * (int64_t)num_cus;
     pl.threads = pairs ? 256 : 512;
     int64_t want = (pairs ? 2 : 1) * num_cus / blocks;
     if (blocks > 1 && want > 8)
@@ -283,7 +289,7 @@ int plan_mfma(const ta_tensor *out, const ta_opts *opts, int num_cus, TAProblem 
     const int64_t groups = lists * blocks;
     const int line = 4 * groups >= 3 * num_cus ? 32 : p.basic ? 30 : p.ks_rows == 64 ? 14 : 7;
     if (num_splits == 0 && item_cost == 0 && lists > 0 && p.merge_kind != TA_MERGE_GENERAL && tiles_cap / lists <= line)
-        p.solo = groups <= num_cus ? TA_SOLO_WIDE : p.basic || (pairs && groups <= 2 * num_cus) ? TA_SOLO_PAIR : 0;
+        p.solo = groups <= num_cus ? TA_SOLO_WIDE : p.basic || (small_blocks && groups <= 2 * num_cus) ? TA_SOLO_PAIR : 0;
     if (p.solo)
         pl.merge_wgs = 0;
     return TA_OK;
@@ -543,6 +549,7 @@ int ta_host_build_q8_problem(const ta_tensor *q, const ta_tensor *k, const ta_te
 const TAQ8Params &ta_host_q8_params(TAQ8Problem *qp)
 {
     static_cast<TAParams &>(qp->p) = qp->pr.p;
+    qp->p.waves = qp->pr.plan.threads / TA_WAVE;
     return qp->p;
 }
 

@@ -702,10 +702,13 @@ hipError_t ta_launch_q8_tile(const TAQ8Params &p, hipStream_t stream, int dev)
         constexpr bool F32 = decltype(f32)::value;
         if (p.solo == TA_SOLO_WIDE)
             return launch_tile<D, W, 8, QT_SOLO, F32>(p, stream, dev);
-        constexpr int NW = W == 8 || F32 ? 8 : 4;
-        if (p.solo)
-            return NW == 4 ? launch_tile<D, W, NW, QT_SOLO, F32>(p, stream, dev) : hipErrorInvalidValue;
-        return launch_tile<D, W, NW, QT_CUT, F32>(p, stream, dev);
+        if constexpr (W < 8 && !F32) {
+            if (p.solo)
+                return launch_tile<D, W, 4, QT_SOLO, F32>(p, stream, dev);
+            if (p.waves == 4)
+                return launch_tile<D, W, 4, QT_CUT, F32>(p, stream, dev);
+        }
+        return p.solo || p.waves != 8 ? hipErrorInvalidValue : launch_tile<D, W, 8, QT_CUT, F32>(p, stream, dev);
     };
     auto rows = [&](auto dh) {
         if (!p.is_bf16)
