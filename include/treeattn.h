@@ -439,7 +439,8 @@ int tree_attn_q8_compact(ta_tensor *k_cache, ta_tensor *v_cache, ta_tensor *k_sc
  * writes the tree tokens); kernel TA_KERNEL_GENERIC names the scalar kernel, TA_KERNEL_MFMA (or _BASIC) the matrix-core one, which
  * takes head_dim 64 or 128, pages of a power of two of at least 16 tokens or contiguous, 16-byte aligned q, K and V rows, cache
  * strides below 2^31, and at most 256 query heads per KV head.
- * A NaN among the codes or scales that a row attends to makes it NaN; one that it does not attend to changes nothing.
+ * A NaN among the codes or scales that a row attends to makes it NaN, and so may a value past the largest bf16 number; one that
+ * it does not attend to changes nothing.
  */
 int tree_attn_q8_fwd(const ta_tensor *q, const ta_tensor *k_cache, const ta_tensor *v_cache, const ta_tensor *k_scale,
                      const ta_tensor *v_scale, const ta_tensor *page_table, const ta_tensor *seq_lens,

@@ -54,6 +54,11 @@ __device__ __forceinline__ void qt_lds_barrier()           // (loads into regist
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }
 
+__device__ __forceinline__ uint32_t qt_infinite(uint32_t x)            // is one of two bf16 numbers infinite (or none)?
+{
+    return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
+}
+
 template <int DH, int NW, bool F32>
 struct QtShape {
     static constexpr int TOKENS = F32 && DH == 128 ? 64 : 16 * NW;   // of a tile
@@ -363,6 +368,11 @@ __global__ __launch_bounds__(64 * NW, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS,
 #pragma unroll
                     for (int n = 0; n < 4; ++n)
                         nan |= ((x.v[i][n] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+                    if (vscale[i] >= 0x1p120f) {           // (a value past the largest number counts as one that is none)
+#pragma unroll
+                        for (int n = 0; n < 4; ++n)
+                            nan |= qt_infinite(q8_bf16_2<false>(x.v[i][n], vscale[i])) | qt_infinite(q8_bf16_2<true>(x.v[i][n], vscale[i]));
+                    }
                     if (mine && pos >= L && nan)
                         atomicOr(nan_nodes, 1ull << (pos - L));
                     if (!mine || (pos >= L && nan)) {

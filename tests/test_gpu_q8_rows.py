@@ -134,3 +134,28 @@ def test_scores_far_apart_and_a_contiguous_cache(T, G, dtype):
     for splits in (0, 1, 4):
         _assert_fwd(_fwd(c, q, torch.from_numpy(par).cuda(), num_splits=splits), want, dtype == "bf16", splits)
     assert ta.tree_attn_last_status() == 0
+
+
+@pytest.mark.parametrize("dtype,kernel", [("bf16", 0), ("f32", 0), ("bf16", 1), ("f32", 1)])
+@pytest.mark.parametrize("T,G,D", [(6, 4, 128), (40, 1, 128), (25, 4, 64), (60, 3, 128)])
+def test_values_past_the_largest_number_in_the_tree(T, G, D, dtype, kernel):
+    """448 * 2^127 as a key's or a value's column of one node: rows that do not attend to it are as without it."""
+    _say("largest", T, G, D, dtype, kernel)
+    B, Hkv, lens = 2, 2, [100, 37]
+    c, q, qh, parent, par = _problem(B, T, G, Hkv, D, 16, lens, 5, dtype)
+    want = ref.expect_fwd(c, qh, par)
+    node = [int(ref.seen_matrix(T, 0, par[b]).sum(0).argmin()) for b in range(B)]      # a leaf
+    for b, (codes, scales) in enumerate(((c.vc0, c.vs0), (c.kc0, c.ks0))):
+        pg, sl = c.place(b, lens[b] + node[b])
+        scales[pg, :, sl] = 254
+        codes[pg, :, sl] = 0
+        codes[pg, :, sl, 3] = 0x7e
+    c.up()
+    for splits in (0, 2):
+        out, lse = _fwd(c, q, parent, num_splits=splits, kernel=kernel)
+        for b in range(B):
+            rows = ~ref.seen_matrix(T, 0, par[b])[:, node[b]]
+            d = np.abs(out[b].double().cpu().numpy() - want[0][b])[rows]
+            assert (d <= ref.bound_fwd(want[0], want[2], dtype == "bf16")[b][rows]).all(), (b, splits)
+            assert np.abs(lse[b].double().cpu().numpy() - want[1][b])[:, rows].max() <= 1e-4
+    assert ta.tree_attn_last_status() == 0
