@@ -217,10 +217,10 @@ int plan_mfma(const ta_tensor *out, const ta_opts *opts, int num_cus, TAProblem 
     const int64_t tiles_cap = lists * ((p.capacity - p.T + TA_TILE - 1) / TA_TILE + 1);
     pl.kernel = TA_KERNEL_MFMA;
     // Query rows of a workgroup.  Up to 32 have a kernel of their own (ta_q8_attn.hip: every wave for itself).  More of them
-    // take tiles of 64, 128 or 256 rows, those that cost least: a pass over the keys takes 107, 178 and 308, relative to one another
-    // (256 rows, 4 requests of 131072 tokens: 856, 712 and 617 us, and 961 in blocks of 32; 64 rows, 32 requests of 8192 tokens: 90, 113
-    // and 168 us, and 101).
-    const int sizes[3] = {64, 128, 256}, costs[3] = {107, 178, 308};
+    // take tiles of 64, 128 or 256 rows, those that cost least: a pass over the keys takes 109, 179 and 302, relative to one another
+    // (256 rows, 4 requests of 131072 tokens: 872, 714 and 604 us, and 961 in blocks of 32; 320 rows, 8 requests of 32768: 540, 504 and
+    // 550; 64 rows, 32 requests of 512 to 8192 tokens: 80, 110 and 168 us, and 101).
+    const int sizes[3] = {64, 128, 256}, costs[3] = {109, 179, 302};
     p.ks_rows = p.is_bf16 ? 32 : 128;
     for (int64_t i = 0, least = INT64_MAX; p.is_bf16 && p.rows > 32 && i < 3; ++i) {
         const int64_t cost = (int64_t)((p.rows + sizes[i] - 1) / sizes[i]) * costs[i];
@@ -242,7 +242,6 @@ int plan_mfma(const ta_tensor *out, const ta_opts *opts, int num_cus, TAProblem 
     p.pad = pl.item_cost - 1;
     if (tiles_cap + lists * p.pad > INT32_MAX)
         return TA_ERR_SHAPE;
-    // workgroups side by side, one grid row apart, should fall on one XCD, where the keys come out of the L2 for all but the first
     // Workgroups of four waves, two on a compute unit, wait for one another less, and take more shares, each with its start and its
     // partial results: 64 rows, 64 requests of 8 KV heads, 512 to 4096 tokens 52 us, 60 with eight waves; 32 of 512 to 8192: 84 and
     // 88; but 8 of 4096: 31 and 29, and 128 rows in one request of 8192: 34 and 31.  (Up to 32 rows: 128 requests, one new token 112 us,
@@ -251,7 +250,7 @@ int plan_mfma(const ta_tensor *out, const ta_opts *opts, int num_cus, TAProblem 
     pl.threads = pairs ? 256 : 512;
     int64_t want = (pairs ? 2 : 1) * num_cus / blocks;
     if (blocks > 1 && want > 8)
-        want -= want % 8;
+        want -= want % 8;                                   // (blocks of the same keys on one XCD, where the L2 has them for all but the first)
     pl.n_wg = (int)(num_splits > 0 ? num_splits : want > 0 ? want : 1);
     if (pl.n_wg > tiles_cap)
         pl.n_wg = (int)(tiles_cap > 0 ? tiles_cap : 1);

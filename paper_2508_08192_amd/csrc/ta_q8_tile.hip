@@ -1,10 +1,11 @@
 // KV pass over the 8-bit cache for many query rows, and for fp32 queries (gfx950): head_dim 64 or 128, fp32 accumulation.
 //
-// A workgroup of eight waves keeps 32 RBW rows (64, 128 or 256) of one (request, KV head) and walks its share in tiles of 128 tokens.
-// The codes of a tile become bf16 values once per workgroup: every wave loads sixteen tokens' codes and scales into registers two
-// tiles ahead, turns them into values (scales and all: a power of two leaves them exact) on their way into LDS one tile ahead, and
-// then multiplies its 32 rows with its part of the tile that all have written: wave w has rows 32 (w % RBW) .. and, of each tile's
-// four runs of 32 tokens, those that are w / RBW modulo 8 / RBW.  Two tiles lie in LDS, one barrier per tile.
+// A workgroup of NW waves (eight, or four of which two share a compute unit) keeps 32 RBW rows (64, 128 or 256) of one (request, KV
+// head) and walks its share in tiles of 16 NW tokens.  The codes of a tile become bf16 values once per workgroup: every wave has
+// its sixteen tokens' codes and scales on the way into registers for two tiles, turns them into values (scales and all: a power of two
+// leaves them exact) on their way into LDS one tile ahead, and then multiplies its 32 rows with its part of the tile that all have written:
+// wave w has rows 32 (w % RBW) .., and of the tile's runs of 32 tokens those that are w / RBW modulo NW / RBW.  Two tiles
+// lie in LDS, one barrier per tile.
 //
 //     S^T[token, row] = K . Q^T ;  O^T[d, row] += V^T . P^T       (as in ta_mfma_ks.hip, on v_mfma_f32_32x32x16_bf16)
 //
@@ -16,11 +17,15 @@
 // are, so three matrix products give what one in fp32 would.  Their first terms of Q stay in registers, the others in LDS, which
 // leaves room for tiles of 64 tokens at head_dim 128.  Not taken: the fp32 matrix instruction, a sixteenth of the bf16 one's rate.
 //
-// Two waves share a SIMD, w and w + 4, and one of them converts before its products, the other behind them (606 us without, at the
-// size below).  What bounds it is the matrix cores and the exponentials' unit in turn: 256 rows, 4 requests of 131072 tokens, 8 KV heads
-// take 594 to 617 us, 890 to 925 TFLOP/s, where a square product of 8192 in bf16 reaches 1200.  Not faster: waves of 64 rows, which
-// read half as many bytes of K and V from LDS, but have no registers left for all of Q (657 us); two groups of waves
-// that take turns at the matrix cores, with a barrier at every turn (695 us).
+// What bounds it, and what it takes (with the merge):
+//   256 rows, 4 requests of 131072 tokens, 8 KV heads: 604 us, 911 TFLOP/s, where a square product of 8192 in bf16 reaches 1200;
+//       the matrix cores, with the exponentials and the LDS reads of a wave only partly under the other wave's products.
+//   64 rows, 32 requests of 512 to 8192 tokens: 80 us, 3.7 TB/s; the chain of a tile's steps in each of two waves per SIMD (a tile of 64
+//       tokens takes a wave some 3000 cycles, 900 of them conversions and 1450 scores, exponentials and products); it is hardly
+//       faster when all pages lie in the L2.
+// Not faster: waves of 64 rows, which read half as many bytes of K and V from LDS, but have no registers left for all of Q (657 us
+// for the first); two groups of waves that take turns at the matrix cores with a barrier at every turn (695); conversions placed
+// between the products of the scores (610, and 87 for the second).
 #include <type_traits>
 
 #include "ta_q8.h"
