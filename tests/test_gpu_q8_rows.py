@@ -159,3 +159,18 @@ def test_values_past_the_largest_number_in_the_tree(T, G, D, dtype, kernel):
             assert (d <= ref.bound_fwd(want[0], want[2], dtype == "bf16")[b][rows]).all(), (b, splits)
             assert np.abs(lse[b].double().cpu().numpy() - want[1][b])[:, rows].max() <= 1e-4
     assert ta.tree_attn_last_status() == 0
+
+
+@pytest.mark.parametrize("dtype,T,G", [("bf16", 8, 4), ("bf16", 16, 4), ("bf16", 64, 2), ("bf16", 64, 4), ("bf16", 64, 7), ("f32", 16, 4)])
+@pytest.mark.parametrize("D,ps", [(128, 16), (128, 64), (64, 32)])
+def test_long_shares(dtype, T, G, D, ps):
+    """Shares of more tiles than a wave holds page ids for, so that it fetches them anew on the way; pages in no order."""
+    _say("long", dtype, T, G, D, ps)
+    B, Hkv, lens = 2, 1, [20001, 8200]
+    c, q, qh, parent, par = _problem(B, T, G, Hkv, D, ps, lens, T, dtype)
+    starts = np.asarray([3000, 77], dtype=np.int32)
+    for kw, args in (({}, {}), (dict(starts=starts), dict(kv_start=torch.from_numpy(starts).cuda()))):
+        want = ref.expect_fwd(c, qh, par, **kw)
+        for splits in (0, 1, 2):
+            _assert_fwd(_fwd(c, q, parent, num_splits=splits, **args), want, dtype == "bf16", splits)
+    assert ta.tree_attn_last_status() == 0
