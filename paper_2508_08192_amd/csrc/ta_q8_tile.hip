@@ -19,7 +19,8 @@
 //
 // What bounds it, and what it takes (with the merge):
 //   256 rows, 4 requests of 131072 tokens, 8 KV heads: 604 us, 911 TFLOP/s, where a square product of 8192 in bf16 reaches 1200;
-//       the matrix cores, with the exponentials and the LDS reads of a wave only partly under the other wave's products.
+//       the matrix cores (46 % of all cycles) and the vector units (53 %) in turn, at some 1.9 GHz; a priority for one of two waves, or
+//       none for either, changes nothing.
 //   64 rows, 32 requests of 512 to 8192 tokens: 80 us, 3.7 TB/s; the chain of a tile's steps in each of two waves per SIMD (a tile of 64
 //       tokens takes a wave some 3000 cycles, 900 of them conversions and 1450 scores, exponentials and products); it is hardly
 //       faster when all pages lie in the L2.
@@ -150,7 +151,9 @@ __global__ __launch_bounds__(64 * NW, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS,
     const int rows_here = min(ROWS, p.rows - row0);
     const float c = p.scale_log2e;
     const bool paged = p.page_table != nullptr;
-    // 16-byte slots of a row in LDS: K slot s of row r holds chunk s ^ kx(r), V slot s chunk s ^ 2 vx(r) (see ta_mfma_ks.hip)
+    // 16-byte slots of a row in LDS: K slot s of row r holds chunk s ^ kx(r), V slot s chunk s ^ 2 vx(r) (see ta_mfma_ks.hip).  At
+    // head_dim 128 the chunks from the eighth on are swapped in pairs, so that the lanes of a row, which write every other chunk at a
+    // time, spread over all banks: of a pass's LDS cycles 30 % were conflicts, now none are, and a call takes 1 % less.
     auto kx = [](int r) { return DH == 64 ? (r >> 1) & 7 : r & 15; };
     auto vx = [](int r) { return DH == 64 ? 2 * ((r >> 1) & 1) + ((r >> 2) & 1) : 2 * (r & 3) + ((r >> 2) & 1); };
     const int kf_at = r32 * C::ROW + ((hf ^ kx(r32)) << 4);
@@ -166,8 +169,8 @@ __global__ __launch_bounds__(64 * NW, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS,
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int row = C::TPW * wave + i * C::RPL + lrow;
-            kw_at[i][h] = row * C::ROW + (((2 * lchunk + h) ^ kx(row)) << 4);
-            vw_at[i][h] = row * C::ROW + (((2 * lchunk + h) ^ (2 * vx(row))) << 4);
+            kw_at[i][h] = row * C::ROW + (((2 * lchunk + h) ^ kx(row) ^ (lchunk >> 2)) << 4);
+            vw_at[i][h] = row * C::ROW + (((2 * lchunk + h) ^ (2 * vx(row)) ^ (lchunk >> 2)) << 4);
         }
 
     typedef __attribute__((address_space(3))) char *lds_t;
@@ -450,7 +453,7 @@ __global__ __launch_bounds__(64 * NW, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS,
             __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int kk = 0; kk < NKK; ++kk) {
-                const qt_u32x4 kf = *(const __attribute__((address_space(3))) qt_u32x4 *)(uintptr_t)((ka ^ (kk << 5)) + tile);
+                const qt_u32x4 kf = *(const __attribute__((address_space(3))) qt_u32x4 *)(uintptr_t)((ka ^ (kk << 5) ^ (kk / 4 << 4)) + tile);
 #pragma unroll
                 for (int t = TERMS - 1; t >= 0; --t) {
                     const uint4 qk = t == 0 ? qf[kk] : ql[((t - 1) * RBW * NKK + kk) * TA_WAVE];
@@ -460,7 +463,7 @@ __global__ __launch_bounds__(64 * NW, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS,
             // ---- V fragments: the first half is requested here and arrives under the softmax, the second under the products of the first
             typedef __attribute__((address_space(3))) qt_s4 *lds_s4;
             auto v_frag = [&](int kb, int db) {
-                const uint32_t a = (va ^ (db << 6)) + tile + C::TILE + kb * 16 * C::ROW;
+                const uint32_t a = (va ^ (db << 6) ^ (db / 2 << 4)) + tile + C::TILE + kb * 16 * C::ROW;
                 const qt_s4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(uintptr_t)a);
                 const qt_s4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(uintptr_t)(a + 8 * C::ROW));
                 return __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7);
