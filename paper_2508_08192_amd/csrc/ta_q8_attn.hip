@@ -95,14 +95,14 @@ __device__ __forceinline__ void q8_dma_s(const void *base, uint32_t off, uint32_
 // Two or four such loads in a row, 1 KB apart in memory and in LDS (the instruction's offset counts on both sides).
 __device__ __forceinline__ void q8_dma_2k(const void *base, uint32_t o0, uint32_t o1, uint32_t lds_wave_base)
 {
-    Q8_DMA("global_load_lds_dwordx4 %[o], %[b] nt\n\tglobal_load_lds_dwordx4 %[p], %[b] offset:1024 nt",
+    Q8_DMA("global_load_lds_dwordx4 %[o], %[b] nt\n\tglobal_load_lds_dwordx4 %[p], %[b] offset:0x400 nt",
            [o] "v"(o0), [p] "v"(o1), [b] "s"(base), [m] "s"(lds_wave_base));
 }
 
 __device__ __forceinline__ void q8_dma_4k(const void *base, uint32_t o0, uint32_t o1, uint32_t lds_wave_base)
 {
-    Q8_DMA("global_load_lds_dwordx4 %[o], %[b] nt\n\tglobal_load_lds_dwordx4 %[p], %[b] offset:1024 nt\n\t"
-           "global_load_lds_dwordx4 %[o], %[b] offset:2048 nt\n\tglobal_load_lds_dwordx4 %[p], %[b] offset:3072 nt",
+    Q8_DMA("global_load_lds_dwordx4 %[o], %[b] nt\n\tglobal_load_lds_dwordx4 %[p], %[b] offset:0x400 nt\n\t"
+           "global_load_lds_dwordx4 %[o], %[b] offset:0x800 nt\n\tglobal_load_lds_dwordx4 %[p], %[b] offset:0xc00 nt",
            [o] "v"(o0), [p] "v"(o1), [b] "s"(base), [m] "s"(lds_wave_base));
 }
 
