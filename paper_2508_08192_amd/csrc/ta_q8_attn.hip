@@ -802,7 +802,7 @@ hipError_t ta_launch_q8_mfma(const TAQ8Params &p, hipStream_t stream, int dev)
 {
     if (dev < 0 || dev >= 64)
         return hipErrorInvalidDevice;
-    if (p.ks_rows != 32 || p.rows > 32 || (!p.solo && p.rows_grp != 32) || !p.part_q15 || p.ls != 2 || !p.is_bf16 || p.direct)
+    if (p.ks_rows != 32 || p.rows > 32 || (!p.solo && p.rows_grp != p.rows) || !p.part_q15 || p.ls != 2 || !p.is_bf16 || p.direct)
         return hipErrorInvalidValue;
     auto rows = [&](auto dh) {
         constexpr int D = decltype(dh)::value;

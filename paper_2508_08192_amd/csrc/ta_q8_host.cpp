@@ -234,7 +234,7 @@ int plan_mfma(const ta_tensor *out, const ta_opts *opts, int num_cus, TAProblem 
     pl.ks_rows = p.ks_rows;
     p.basic = p.ks_rows == 32;
     const int blocks = (p.rows + p.ks_rows - 1) / p.ks_rows;
-    p.rows_grp = pl.rows_grp = blocks * p.ks_rows;
+    p.rows_grp = pl.rows_grp = p.rows;
     p.n_rg = pl.n_rg = 1;
     // (what a share of a list costs beside its tiles: 128 requests of 8 KV heads, one new token, 15 105 us, 9 117; 20 costs 1 % more.
     // With tiles for all waves 9 to 13 are the same within 2 %.)

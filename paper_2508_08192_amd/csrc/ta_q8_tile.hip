@@ -712,7 +712,7 @@ hipError_t ta_launch_q8_tile(const TAQ8Params &p, hipStream_t stream, int dev)
 {
     if (dev < 0 || dev >= 64)
         return hipErrorInvalidDevice;
-    if (p.direct || (!p.solo && p.rows_grp % p.ks_rows != 0) || p.part_q15 != p.is_bf16 || p.ls != (p.is_bf16 ? 2 : 1) ||
+    if (p.direct || (!p.solo && p.rows_grp != p.rows) || p.part_q15 != p.is_bf16 || p.ls != (p.is_bf16 ? 2 : 1) ||
         (!p.is_bf16 && p.ks_rows != 128))
         return hipErrorInvalidValue;
     auto with = [&](auto dh, auto rbw, auto f32) {
