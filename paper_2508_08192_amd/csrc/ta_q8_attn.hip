@@ -17,7 +17,7 @@
 // The scales of a run, K's and V's, come with one load of a byte per lane ahead of V's codes.
 //
 // What bounds it: the loads.  128 requests of 8192 tokens, 8 KV heads, one new token with 4 heads each: 341 us with the merge, 6.3 TB/s,
-// where a plain streaming read reaches 6.8; of 256 to 4096 tokens 105 us, 5.5 TB/s.  One request of 8192 tokens, one KV head: 14 us,
+// where a plain streaming read reaches 6.8; of 256 to 4096 tokens 103 us, 5.6 TB/s.  One request of 8192 tokens, one KV head: 14 us,
 // two launches and the round trips of one share.
 #include <initializer_list>
 #include <type_traits>

@@ -18,10 +18,10 @@
 // leaves room for tiles of 64 tokens at head_dim 128.  Not taken: the fp32 matrix instruction, a sixteenth of the bf16 one's rate.
 //
 // What bounds it, and what it takes (with the merge):
-//   256 rows, 4 requests of 131072 tokens, 8 KV heads: 604 us, 911 TFLOP/s, where a square product of 8192 in bf16 reaches 1200;
+//   256 rows, 4 requests of 131072 tokens, 8 KV heads: 597 us, 921 TFLOP/s, where a square product of 8192 in bf16 reaches 1200;
 //       the matrix cores (46 % of all cycles) and the vector units (53 %) in turn, at some 1.9 GHz; a priority for one of two waves, or
 //       none for either, changes nothing.
-//   64 rows, 32 requests of 512 to 8192 tokens: 80 us, 3.7 TB/s; the chain of a tile's steps in each of two waves per SIMD (a tile of 64
+//   64 rows, 32 requests of 512 to 8192 tokens: 79 us, 3.8 TB/s; the chain of a tile's steps in each of two waves per SIMD (a tile of 64
 //       tokens takes a wave some 3000 cycles, 900 of them conversions and 1450 scores, exponentials and products); it is hardly
 //       faster when all pages lie in the L2.
 // Not faster: waves of 64 rows, which read half as many bytes of K and V from LDS, but have no registers left for all of Q (657 us
