@@ -229,8 +229,8 @@ int plan_mfma(const ta_tensor *out, const ta_opts *opts, int num_cus, TAProblem 
             p.ks_rows = sizes[i];
         }
     }
-    // (fp32 queries, each the sum of three bf16 numbers, have blocks of 128 rows: 128 requests with 8 rows and 8192 tokens 168 us, and
-    // 1674 with the scalar kernel; 32 requests with 64 rows, 8 KV heads, 4096 tokens 177 and 6560)
+    // (fp32 queries, each the sum of three bf16 numbers, have blocks of 128 rows: 128 requests with 8 rows and 8192 tokens 120 us, and
+    // 1670 with the scalar kernel; 32 requests with 64 rows, 8 KV heads, 4096 tokens 130 and 6540)
     pl.ks_rows = p.ks_rows;
     p.basic = p.ks_rows == 32;
     const int blocks = (p.rows + p.ks_rows - 1) / p.ks_rows;
@@ -244,9 +244,12 @@ int plan_mfma(const ta_tensor *out, const ta_opts *opts, int num_cus, TAProblem 
         return TA_ERR_SHAPE;
     // Workgroups of four waves, two on a compute unit, wait for one another less, and take more shares, each with its start and its
     // partial results: 64 rows, 64 requests of 8 KV heads, 512 to 4096 tokens 52 us, 60 with eight waves; 32 of 512 to 8192: 84 and
-    // 88; but 8 of 4096: 31 and 29, and 128 rows in one request of 8192: 34 and 31.  (Up to 32 rows: 128 requests, one new token 112 us,
+    // 88; but 8 of 4096: 31 and 29, and 128 rows in one request of 8192: 34 and 31.  With no more tiles than workgroups every share is one
+    // of the smaller tiles: 64 rows in one list of 8192 tokens 16.4 us, 18.1 with eight waves, 8 lists of 2048 17.7 and 19.5; 16 of 2000, which
+    // are past the line, 20.0 and 19.9.  (Up to 32 rows: 128 requests, one new token 112 us,
     // 105 with eight waves.)
-    const bool small_blocks = p.is_bf16 && (p.ks_rows == 64 || p.ks_rows == 128), pairs = small_blocks && tiles_cap >= 64 * (int64_t)num_cus;
+    const bool small_blocks = p.is_bf16 && (p.ks_rows == 64 || p.ks_rows == 128);
+    const bool pairs = small_blocks && (tiles_cap >= 64 * (int64_t)num_cus || tiles_cap <= num_cus + num_cus / 4);
     pl.threads = pairs ? 256 : 512;
     int64_t want = (pairs ? 2 : 1) * num_cus / blocks;
     if (blocks > 1 && want > 8)
@@ -274,19 +277,19 @@ int plan_mfma(const ta_tensor *out, const ta_opts *opts, int num_cus, TAProblem 
     pr->ws_ls_off = p.part_q15 ? ta_host_align_up(rows_total * p.D * 2, 256) : pr->ws_o_bytes;
     pr->ws_bytes = pr->ws_o_bytes + pr->ws_lse_bytes + ta_host_align_up((size_t)lists * 2 * sizeof(int32_t), 256);
     // Short lists go to one workgroup each, which writes the outputs itself: no schedule, no partial results, no merge pass.  Up to
-    // how many tiles depends on what a tile takes the workgroup, and on how many stand idle meanwhile (us per call, uncut / cut):
-    //     rows        8 lists                     64 lists                    256 lists
-    //     32          24 tiles 12.0/13.0          32 tiles 14.0/16.9          32 tiles 16.6/22.0
-    //                 48       16.0/13.3          64       20.3/16.7          64       26.3/31.9
-    //     64           8       14.0/15.9          16       18.3/19.3          32       27.2/30.9
-    //                 16       17.8/16.1          24       21.8/19.5          64       42.1/43.0
-    //     256          4       21.8/26.5           8       27.1/29.8          32       60.3/72.9
-    //                  8       26.5/25.4          24       44.5/33.2          64       96.7/105.6
-    //     fp32         4       13.3/17.2           8       19.0/21.6          24       40.7/42.4
-    //                  8       18.6/18.2          16       28.9/24.4          48       71.8/69.9
-    // (A batch of uneven lengths waits for its longest list: the line for a full chip stays where the gain is a fifth.)
+    // how many tiles depends on what a tile takes the workgroup, and on how many stand idle meanwhile (tokens, us uncut / cut):
+    //     rows        8 lists                64 lists               256 lists
+    //     32          1024  13.2/13.3        1024  14.0/16.9        1024  16.6/22.0
+    //                 1536  16.0/13.3        1536  16.6/16.5        2048  26.3/31.9
+    //     64           256  14.0/15.9         512  18.3/19.3        1024  27.2/30.9
+    //                  512  17.8/16.1         768  21.8/19.5        2048  42.1/43.0
+    //     256          128  21.8/26.5         256  27.1/29.8        1024  60.3/72.9
+    //                  256  26.5/25.4         768  44.5/33.2        2048  96.7/105.6
+    //     fp32         256  16.5/17.5         256  16.9/20.1        1024  38.9/41.5
+    //                  768  38.2/16.6         768  38.5/27.1        1536  52.7/54.1
+    // (A batch of uneven lengths waits for its longest list: the line for a full chip stays where the gain is a tenth and more.)
     const int64_t groups = lists * blocks;
-    const int line = 4 * groups >= 3 * num_cus ? 32 : p.basic ? 30 : p.ks_rows == 64 ? 14 : 7;
+    const int line = 4 * groups >= 3 * num_cus ? 32 : p.basic ? 18 : p.ks_rows == 64 ? 8 : 5;
     if (num_splits == 0 && item_cost == 0 && lists > 0 && p.merge_kind != TA_MERGE_GENERAL && tiles_cap / lists <= line)
         p.solo = groups <= num_cus ? TA_SOLO_WIDE : p.basic || (small_blocks && groups <= 2 * num_cus) ? TA_SOLO_PAIR : 0;
     if (p.solo)

@@ -105,7 +105,7 @@ __global__ __launch_bounds__(64 * NW, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS,
     const TASched sc = TA_SCHED;
     using C = QtShape<DH, NW, F32>;
     constexpr bool SOLO = MODE == QT_SOLO;
-    constexpr int KW = NW / RBW, NR = C::TOKENS / 32 / KW;                             // waves that share rows, runs of a tile for each of them
+    constexpr int KW = NW / RBW, NR = C::TOKENS / 32 / KW, WSTEP = F32 ? 1 : RBW;      // waves that share rows, runs of a tile for each of them, from one to the next
     constexpr int TERMS = F32 ? 3 : 1;                                   // bf16 numbers whose sum is a query's or a probability's
     constexpr int NKK = DH / 16, NDB = DH / 32, NL = C::NL, ROWS = 32 * RBW;
     extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -118,7 +118,7 @@ __global__ __launch_bounds__(64 * NW, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS,
     const int tid = threadIdx.x, lane = tid & 63;
     const int w = blockIdx.x, row0 = blockIdx.y * ROWS;                  // first of the workgroup's query rows
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int rb = wave % RBW, kg = wave / RBW;
+    const int rb = F32 ? wave / KW : wave % RBW, kg = F32 ? wave % KW : wave / RBW;
     const int r32 = lane & 31, hf = lane >> 5;
     // schedule, as in ta_q8_attn.hip
     const bool in_regs = sc.B <= TA_WAVE;
@@ -149,6 +149,9 @@ __global__ __launch_bounds__(64 * NW, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS,
         t_end = __builtin_amdgcn_readfirstlane(t_end);
     }
     const int rows_here = min(ROWS, p.rows - row0);
+    // (fp32: a wave without rows only loads and converts for the others.  128 requests with 8 rows 120 us, 164 with products of rows
+    // that nobody asked for; with no more than 64 rows those that have any lie on SIMDs of their own.)
+    const int n_runs = !F32 || 32 * rb < rows_here ? NR : 0;
     const float c = p.scale_log2e;
     const bool paged = p.page_table != nullptr;
     // 16-byte slots of a row in LDS: K slot s of row r holds chunk s ^ kx(r), V slot s chunk s ^ 2 vx(r) (see ta_mfma_ks.hip).  At
@@ -550,7 +553,7 @@ __global__ __launch_bounds__(64 * NW, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS,
             write_tile(j + 1, C::BUF - BUF, next);
             load_tile(j + 3, next);
 #pragma unroll 1
-            for (int r = 0; r < NR; ++r) {
+            for (int r = 0; r < n_runs; ++r) {
                 const int at = 32 * (kg + KW * r), pos0 = base + j * C::TOKENS + at;
                 if (pos0 < end && pos0 + 32 > first)
                     run(BUF, at, pos0);
@@ -603,11 +606,11 @@ __global__ __launch_bounds__(64 * NW, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS,
         constexpr int CPT = DH / 16;                       // columns of a thread: sixteen of them per row
 #pragma unroll 1
         for (int row = tid / 16; row < ROWS; row += 4 * NW) {
-            const int c0 = (tid % 16) * (CPT / 4), rr = row & 31, wv0 = row / 32;
+            const int c0 = (tid % 16) * (CPT / 4), rr = row & 31, wv0 = F32 ? row / 32 * KW : row / 32;       // the first wave of its rows
             float mw[KW], big = -INFINITY;
 #pragma unroll
             for (int k = 0; k < KW; ++k) {
-                mw[k] = stat[((wv0 + k * RBW) * 2 + 0) * 32 + rr];
+                mw[k] = stat[((wv0 + k * WSTEP) * 2 + 0) * 32 + rr];
                 big = fmaxf(big, mw[k]);
             }
             float l_tot = 0.f, acc[CPT];
@@ -617,10 +620,10 @@ __global__ __launch_bounds__(64 * NW, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS,
 #pragma unroll
             for (int k = 0; k < KW; ++k) {
                 const float wgt = mw[k] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw[k] - big);
-                l_tot = fmaf(wgt, stat[((wv0 + k * RBW) * 2 + 1) * 32 + rr], l_tot);
+                l_tot = fmaf(wgt, stat[((wv0 + k * WSTEP) * 2 + 1) * 32 + rr], l_tot);
 #pragma unroll
                 for (int q = 0; q < CPT / 4; ++q) {
-                    const float4 x = *(const float4 *)(smem + (wv0 + k * RBW) * C::STAGE + (rr * DH + (((c0 + q) ^ (rr & 15)) << 2)) * 4);
+                    const float4 x = *(const float4 *)(smem + (wv0 + k * WSTEP) * C::STAGE + (rr * DH + (((c0 + q) ^ (rr & 15)) << 2)) * 4);
                     acc[4 * q + 0] = fmaf(wgt, x.x, acc[4 * q + 0]);
                     acc[4 * q + 1] = fmaf(wgt, x.y, acc[4 * q + 1]);
                     acc[4 * q + 2] = fmaf(wgt, x.z, acc[4 * q + 2]);
