@@ -174,3 +174,34 @@ def test_long_shares(dtype, T, G, D, ps):
         for splits in (0, 1, 2):
             _assert_fwd(_fwd(c, q, parent, num_splits=splits, **args), want, dtype == "bf16", splits)
     assert ta.tree_attn_last_status() == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,G", [(1, 8), (10, 4), (20, 5), (50, 5)])
+@pytest.mark.parametrize("L", [1000, 8192, 40000])
+def test_one_list(T, G, L, dtype):
+    """One request with one KV head: the split over workgroups and the merge of many parts."""
+    _say("one list", T, G, L, dtype)
+    c, q, qh, parent, par = _problem(1, T, G, 1, 128, 64, [L], L + T, dtype)
+    want = ref.expect_fwd(c, qh, par)
+    for splits in (0, 100, 256):
+        _assert_fwd(_fwd(c, q, parent, num_splits=splits), want, dtype == "bf16", splits)
+    assert ta.tree_attn_last_status() == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_large_batch(dtype):
+    """More requests than a workgroup keeps lengths of, in every kernel, some of them without a token."""
+    _say("large batch", dtype)
+    B = 2100
+    for T, G in ((1, 2), (9, 4)):
+        lens = [(0, 5, 64, 100, 31)[i % 5] for i in range(B)]
+        c, q, qh, parent, par = _problem(B, T, G, 1, 64, 16, lens, T, dtype)
+        got = _fwd(c, q, parent)
+        some = np.random.default_rng(0).choice(B, 60, replace=False)
+        for b in some.tolist():
+            one = ref.Cache.__new__(ref.Cache)
+            one.__dict__.update(c.__dict__)
+            one.lens, one.table = c.lens[b:b + 1], c.table[b:b + 1]
+            _assert_fwd((got[0][b:b + 1], got[1][b:b + 1]), ref.expect_fwd(one, qh[b:b + 1], par[b:b + 1]), dtype == "bf16", b)
+    assert ta.tree_attn_last_status() == 0
