@@ -111,6 +111,7 @@ class TreeAttnError(RuntimeError):
 
 _lib = None
 _call = None                   # the extension module; None without torch, whose tensors are all it takes, or where it is not built
+_current = None                # torch's functions that name the current stream of an initialised process
 _entry = {}                    # addresses of the entry points it calls
 
 
@@ -254,11 +255,15 @@ def _stream_ptr(stream):
 
 def _stream_address(stream):
     """The same as an integer."""
+    global _current
     if stream is None:
-        from torch import _C, cuda
-        if cuda.is_initialized():
-            return _C._cuda_getCurrentRawStream(_C._cuda_getDevice())
-        return cuda.current_stream().cuda_stream
+        if _current is None:                           # (found once: the import statement alone takes 0.3 us a call)
+            from torch import _C, cuda
+            if not cuda.is_initialized():
+                return cuda.current_stream().cuda_stream
+            _current = cuda, _C._cuda_getCurrentRawStream, _C._cuda_getDevice
+        cuda, raw_stream, device = _current
+        return raw_stream(device()) if cuda.is_initialized() else cuda.current_stream().cuda_stream
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream if stream != 0 else 0        # (a zero of any type is the default stream)
