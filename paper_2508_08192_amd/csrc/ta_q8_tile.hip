@@ -36,6 +36,7 @@ typedef float qt_f32x16 __attribute__((ext_vector_type(16)));
 typedef short qt_s4 __attribute__((ext_vector_type(4)));
 typedef short qt_s8 __attribute__((ext_vector_type(8)));
 typedef uint32_t qt_u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t qt_u32x4_8 __attribute__((ext_vector_type(4), aligned(8)));     // (outputs start on 8 bytes)
 
 #define QT_LENS 256                              // batches of up to this many requests keep their lengths in LDS
 
@@ -566,8 +567,9 @@ __global__ __launch_bounds__(64 * NW, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS,
             step(j + 1, std::false_type{}, even);
         }
 
-        // ---- results: each wave stages its 32 x DH block (16-byte chunk ch of row r at chunk ch ^ (r & 15)), then the threads add up
-        // those of the waves that share rows
+        // ---- results.  A wave that shares its rows with no other has all of them in registers.  Otherwise each wave stages its 32 x DH
+        // block (16-byte chunk ch of row r at chunk ch ^ (r & 15)), and the threads add up those of the waves that share rows.
+        constexpr bool ALONE = KW == 1 && !F32;
         {
             int wb = 0;
             if (__any(bad)) {
@@ -583,26 +585,74 @@ __global__ __launch_bounds__(64 * NW, 2) void ta_q8_tile_kernel(TA_SCHED_PARAMS,
                     for (int i = 0; i < 16; ++i)
                         o[db][i] = __uint_as_float(0x7fc00000u);
             }
-            const float l_tot = l_run + __shfl_xor(l_run, 32, TA_WAVE);
-            if (hf == 0) {
-                stat[(wave * 2 + 0) * 32 + r32] = m_run;
-                stat[(wave * 2 + 1) * 32 + r32] = l_tot;
-            }
-            float *stage = (float *)(smem + wave * C::STAGE);
-#pragma unroll
-            for (int db = 0; db < NDB; ++db)
-#pragma unroll
-                for (int i4 = 0; i4 < 4; ++i4) {
-                    const int ch = db * 8 + 2 * i4 + hf;
-                    *(float4 *)(stage + r32 * DH + ((ch ^ (r32 & 15)) << 2)) =
-                        make_float4(o[db][4 * i4], o[db][4 * i4 + 1], o[db][4 * i4 + 2], o[db][4 * i4 + 3]);
+            if constexpr (!ALONE) {
+                const float l_tot = l_run + __shfl_xor(l_run, 32, TA_WAVE);
+                if (hf == 0) {
+                    stat[(wave * 2 + 0) * 32 + r32] = m_run;
+                    stat[(wave * 2 + 1) * 32 + r32] = l_tot;
                 }
+                float *stage = (float *)(smem + wave * C::STAGE);
+#pragma unroll
+                for (int db = 0; db < NDB; ++db)
+#pragma unroll
+                    for (int i4 = 0; i4 < 4; ++i4) {
+                        const int ch = db * 8 + 2 * i4 + hf;
+                        *(float4 *)(stage + r32 * DH + ((ch ^ (r32 & 15)) << 2)) =
+                            make_float4(o[db][4 * i4], o[db][4 * i4 + 1], o[db][4 * i4 + 2], o[db][4 * i4 + 3]);
+                    }
+            }
         }
         qt_lds_barrier();
         int any_bad = 0;
 #pragma unroll
         for (int k = 0; k < NW; ++k)
             any_bad |= wbad[k];
+        if constexpr (ALONE) {
+            const int row = rb * 32 + r32;
+            const float l_tot = l_run + __shfl_xor(l_run, 32, TA_WAVE), inv = any_bad ? 0.f : 1.f / l_tot;
+            uint32_t top = 0;                              // (bits of the row's largest magnitude, as below)
+#pragma unroll
+            for (int db = 0; db < NDB; ++db)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    o[db][i] *= inv;
+                    top = max(top, __float_as_uint(o[db][i]) & 0x7fffffffu);
+                }
+            top = max(top, (uint32_t)__shfl_xor((int)top, 32, TA_WAVE));
+            const bool nan_seen = top > 0x7f800000u;
+            const float amax = nan_seen ? 0.f : __uint_as_float(top);
+            const float lse2 = any_bad ? __uint_as_float(0x7fc00000u) : m_run + log2f(l_tot);
+            float scale, to_q;
+            ta_q15_scale(amax, nan_seen, scale, to_q);
+            const bool nan = any_bad || nan_seen || amax == INFINITY || lse2 != lse2;
+            const int R = row0 + (row < rows_here ? row : 0), node = (int)__umulhi((uint32_t)R << 8, p.g_magic), h = g * p.G + R - node * p.G;
+            const int64_t wrow = SOLO ? 0 : ta_ws_row(p, slot, 0, R);
+            char *const dst = SOLO ? (char *)((uint16_t *)p.out + (int64_t)b * p.o_sb + (int64_t)node * p.o_st + (int64_t)h * p.o_sh)
+                                   : ta_part_row(p, wrow);
+            auto two = [&](float x, float y) { return SOLO ? (nan ? 0x7fc07fc0u : q8_pack_bf16(x, y)) : ta_q15_pack(x, y, to_q); };
+#pragma unroll
+            for (int db = 0; db < NDB; ++db)
+#pragma unroll
+                for (int p2 = 0; p2 < 2; ++p2) {
+                    // the two halves of a row exchange columns: a lane then has eight in a row
+                    const int e = 8 * p2;
+                    const auto w0 = __builtin_amdgcn_permlane32_swap(two(o[db][e], o[db][e + 1]), two(o[db][e + 4], o[db][e + 5]), false, false);
+                    const auto w1 = __builtin_amdgcn_permlane32_swap(two(o[db][e + 2], o[db][e + 3]), two(o[db][e + 6], o[db][e + 7]), false, false);
+                    if (row < rows_here)
+                        *(qt_u32x4_8 *)(dst + 2 * (32 * db + 16 * p2 + 8 * hf)) = qt_u32x4_8{w0[0], w1[0], w0[1], w1[1]};
+                }
+            if (row < rows_here && hf == 0) {
+                if constexpr (!SOLO)
+                    *(float2 *)&p.ws_lse[2 * wrow] = make_float2(lse2, scale);
+                else if (p.lse)
+                    p.lse[(int64_t)b * p.lse_sb + (int64_t)h * p.lse_sh + (int64_t)node * p.lse_st] =
+                        lse2 == -INFINITY ? __uint_as_float(0x7fc00000u) : lse2 * 0.6931471805599453f;
+            }
+            if (any_bad && tid == 0)
+                ta_raise(p, any_bad);
+            qt_lds_barrier();                              // everything has been read
+            continue;
+        }
         constexpr int CPT = DH / 16;                       // columns of a thread: sixteen of them per row
 #pragma unroll 1
         for (int row = tid / 16; row < ROWS; row += 4 * NW) {
