@@ -288,10 +288,18 @@ int plan_mfma(const ta_tensor *out, const ta_opts *opts, int num_cus, TAProblem 
     //     fp32         256  16.5/17.5         256  16.9/20.1        1024  38.9/41.5
     //                  768  38.2/16.6         768  38.5/27.1        1536  52.7/54.1
     // (A batch of uneven lengths waits for its longest list: the line for a full chip stays where the gain is a tenth and more.)
-    const int64_t groups = lists * blocks;
-    const int line = 4 * groups >= 3 * num_cus ? 32 : p.basic ? 18 : p.ks_rows == 64 ? 8 : 5;
-    if (num_splits == 0 && item_cost == 0 && lists > 0 && p.merge_kind != TA_MERGE_GENERAL && tiles_cap / lists <= line)
-        p.solo = groups <= num_cus ? TA_SOLO_WIDE : p.basic || (small_blocks && groups <= 2 * num_cus) ? TA_SOLO_PAIR : 0;
+    // More lists than workgroups run at a time take rounds, the last of which may be almost empty.  In tiles, a round takes some 10 and
+    // the list's (8 with two workgroups on a compute unit); cut, a list takes some 15 (20) and its own, and the call 6: 64 rows, 2048 lists
+    // of 200 tokens 68 us uncut, 134 cut, 640 lists of 1000 60 and 74; 256 rows, 400 lists of 500 tokens 77 and 90, 264 lists (two rounds for
+    // eight of them) of 1000 106 and 83.
+    const int64_t groups = lists * blocks, n = lists > 0 ? tiles_cap / lists : 0;
+    const int64_t slots = groups <= num_cus ? num_cus : (p.basic || small_blocks ? 2 : 1) * (int64_t)num_cus;
+    const int64_t rounds = (groups + slots - 1) / slots;
+    const int64_t solo_start = slots > num_cus ? 8 : 10, cut_start = slots > num_cus ? 20 : 15;
+    const int line = 4 * groups >= 3 * slots ? 32 : p.basic || groups > num_cus ? 18 : p.ks_rows == 64 ? 8 : 5;
+    if (num_splits == 0 && item_cost == 0 && lists > 0 && p.merge_kind != TA_MERGE_GENERAL && n <= line &&
+        (rounds == 1 || rounds * (n + solo_start) * slots <= 6 * slots + groups * (n + cut_start)))
+        p.solo = slots == num_cus ? TA_SOLO_WIDE : TA_SOLO_PAIR;
     if (p.solo)
         pl.merge_wgs = 0;
     return TA_OK;
