@@ -18,7 +18,7 @@
 // leaves room for tiles of 64 tokens at head_dim 128.  Not taken: the fp32 matrix instruction, a sixteenth of the bf16 one's rate.
 //
 // What bounds it, and what it takes (with the merge):
-//   256 rows, 4 requests of 131072 tokens, 8 KV heads: 597 us, 921 TFLOP/s, where a square product of 8192 in bf16 reaches 1200;
+//   256 rows, 4 requests of 131072 tokens, 8 KV heads: 590 us, 930 TFLOP/s, where a square product of 8192 in bf16 reaches 1200;
 //       the matrix cores (46 % of all cycles) and the vector units (53 %) in turn, at some 1.9 GHz; a priority for one of two waves, or
 //       none for either, changes nothing.
 //   64 rows, 32 requests of 512 to 8192 tokens: 79 us, 3.8 TB/s; the chain of a tile's steps in each of two waves per SIMD (a tile of 64
